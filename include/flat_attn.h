@@ -249,6 +249,107 @@ int flat_attn_varlen_fwd(const void* Q, const void* K, const void* V, void* O,
                          int max_seqlen_q, float scale, int causal, int32_t* status, void* stream);
 
 /*
+ * Rotary positions (the paper's decoder workloads encode positions; it does not model how).  The first rotary_dim features of
+ * every head are taken in pairs -- (i, i + rotary_dim / 2), or (2 i, 2 i + 1) where `interleaved` is 1 -- and pair i of a token at
+ * position m is rotated by the angle m f_i and multiplied by `amplitude`:
+ *     y1 = amplitude (x1 cos - x2 sin),   y2 = amplitude (x2 cos + x1 sin);   the features behind rotary_dim are passed on.
+ * flat_attn_rope_bwd is the gradient: Q and K take the gradients of the rotated tensors, Qr and Kr receive those of the tensors
+ * before the rotation (the same with sin negated).
+ *
+ * flat_attn_rope_table (HOST only, no device is touched) fills `table` (HOST, rotary_dim / 2 words) with the frequencies, in units
+ * of 2^-64 turns a token, which the caller copies to the device once, and *amplitude (HOST).  f_i = base^(-2 i / rotary_dim), scaled
+ * for contexts longer than the model was trained on:
+ *   FLAT_ROPE_PLAIN   as it is                              FLAT_ROPE_LINEAR  f_i / factor
+ *   FLAT_ROPE_BASE    base * factor^(r / (r - 2)) instead of base, r = rotary_dim (r = 2, whose one frequency is 1: as it is)
+ *   FLAT_ROPE_PARTS   with n_i = original_len f_i / (2 pi), the turns over the original context, and keep = (n_i - low) / (high - low)
+ *                     between 0 and 1:  (1 - keep) f_i / factor + keep f_i, and an amplitude of 0.1 ln(factor) + 1
+ *                     (arXiv 2309.00071; low = 1, high = 32 there)
+ * base > 1 and at most 1e30, 1 <= factor <= 1e6, and for PARTS original_len >= 1 and 0 <= low < high (FLAT_ERR_SHAPE); amplitude is 1 but for PARTS.
+ *
+ * Q, Qr : [B, Hq, N, d]    K, Kr : [B, Hk, N, d], or both NULL (Hk is not read then); d contiguous, the other strides (in elements,
+ * in the order batch, head, token) free: multiples of 16 bytes, >= 0.  Packed tokens are B = 1.  Qr may be Q, and Kr K, with the
+ * same strides; otherwise what is written may overlap nothing else, itself included (an output stride of 0 along more than one
+ * element is FLAT_ERR_SHAPE).  positions: device, position of token n of batch b at b * positions_stride_b + n (a stride of 0 shares
+ * them), any 32-bit value; NULL: token n has position n.  bf16 or fp32; cosines, sines and products in fp32, rounded once.
+ * d in {16, 32, 64, 128}, rotary_dim even, 2 <= rotary_dim <= d (FLAT_ERR_UNSUPPORTED).  B <= 65535, B * N <= 2^31 - 1, (Hq + Hk) <= 65535.
+ * One kernel; pointers 16-byte aligned (positions 4, table 8).  `p` is a HOST pointer, read before the call returns.
+ */
+enum { FLAT_ROPE_PLAIN = 0, FLAT_ROPE_LINEAR = 1, FLAT_ROPE_BASE = 2, FLAT_ROPE_PARTS = 3 };
+int flat_attn_rope_table(int rotary_dim, double base, int scaling, double factor, long long original_len, double low, double high,
+                         uint64_t* table, float* amplitude);
+typedef struct flat_attn_rope_params {
+    const void *Q, *K;
+    void *Qr, *Kr;
+    int B, N, Hq, Hk, d;
+    long long q_stride[3], k_stride[3], qr_stride[3], kr_stride[3];   /* batch, head, token; in elements       */
+    const int32_t* positions;
+    long long positions_stride_b;
+    const uint64_t* table;     /* device, rotary_dim / 2 words                                  */
+    int rotary_dim, interleaved;
+    float amplitude;           /* finite                                                        */
+    int dtype;                 /* FLAT_DTYPE_*                                                  */
+} flat_attn_rope_params_t;
+int flat_attn_rope_fwd(const flat_attn_rope_params_t* p, void* stream);
+int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream);
+
+/*
+ * A cache of keys and values in 8 bits, in pages, and attention over it (the same operators as flat_attn_varlen_fwd: Section 2
+ * steps 2-4 sequence by sequence; the paper has no counterpart for the cache).
+ *   k_cache, v_cache : [num_pages, Hkv, page, d] e4m3 (no infinities; 0x7f and 0xff are NaN)
+ *   k_exp, v_exp     : [num_pages, Hkv] bytes: the values of a page and head are the e4m3 numbers times 2^(exp - 127)
+ *   page_table       : [num_seqs, max_pages] int32, row s the pages of sequence s in order; entries behind its length are not read
+ *   cu_seqlens       : [num_seqs + 1] int32: sequence s owns the new tokens cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (its queries, or the
+ *                      keys and values to append); may own none.  Tokens behind the last sequence are left alone.
+ *   seq_lens         : [num_seqs] int32: tokens of sequence s, the new ones (its last) included
+ * All are device memory, caller-owned.  page in {16, 32, 64, 128}, d in {64, 128} (FLAT_ERR_UNSUPPORTED).  16-byte aligned, the
+ * int32 arrays 4-byte.  max_new >= the new tokens of every sequence (it sizes the grid).
+ * What the device finds wrong in page_table, cu_seqlens and seq_lens faults nothing: a sequence whose offsets do not lie in
+ * 0 .. total, or that has more new tokens than max_new or than its length, or a length beyond max_pages * page, is left out (FLAT_CACHE_BAD_LENGTH in
+ * `status`, its outputs unwritten); a page index outside 0 .. num_pages - 1 is left out with its tokens (FLAT_CACHE_BAD_PAGE).
+ *
+ * flat_attn_cache_append writes the new tokens' K, V [total, Hkv, d] bf16 (strides of token and head in elements, multiples of 8; d
+ * contiguous) to their places.  The exponent of a page and head is the least e >= -117 with max |x| <= 448 * 2^e over the tokens written
+ * to it by this call, and not below what it was where earlier tokens of the sequence share the page: if it grows, those are rounded
+ * again to the new scale.  (Scales are powers of two: a growing scale changes a value only where it becomes subnormal.)  Values are
+ * rounded to nearest even.  Infinities and NaN are written as NaN and do not count for the exponent.  Pages that a call writes to must belong
+ * to one sequence each.  K and V are read once, 2 bytes a token and feature are written.
+ *
+ * flat_attn_cache_fwd: Q, O [total, Hq, d] bf16 (strides as above), Hq = G * Hkv: query head h reads key head h / G, G <= 128.  causal = 1:
+ * query i of n sees the keys j <= i + length - n; 0: all of its sequence.  O = 0 (and lse = -inf) for a row whose keys are all left out.
+ * Cache entries of a sequence must be finite; what lies behind its length in its last page is ignored, NaN included.
+ * lse: optional [total, Hq] fp32, as in flat_attn_params_t.  Keys and values are used unrounded (e4m3 is exact in the half
+ * precision of the products), Q as half-precision numbers scaled by a power of two for each row (unrounded where a feature is within 2^-28 of
+ * the row's largest), weights rounded to half precision, sums in fp32.  The keys of long sequences are split over CTAs and joined in a fixed order: same bits every time.
+ * workspace: device, at least flat_attn_cache_workspace_bytes(Hq, Hkv, d) bytes on the device of the call, 256-byte aligned, zeroed once by the caller; every call
+ * leaves it ready for the next.  Calls that may run at the same time (other streams, captured graphs that overlap) need one each.
+ */
+#define FLAT_CACHE_BAD_PAGE 0xb00
+#define FLAT_CACHE_BAD_LENGTH 0xb01
+typedef struct flat_attn_cache {
+    void *k_cache, *v_cache;
+    uint8_t *k_exp, *v_exp;
+    const int32_t *page_table, *cu_seqlens, *seq_lens;
+    int num_pages, Hkv, page, d;
+    int num_seqs, max_pages;
+    int32_t* status;           /* optional device word, as in flat_attn_params_t                */
+} flat_attn_cache_t;
+int flat_attn_cache_append(const flat_attn_cache_t* c, const void* K, const void* V, long long total, long long k_stride_t,
+                           long long k_stride_h, long long v_stride_t, long long v_stride_h, int max_new, void* stream);
+typedef struct flat_attn_cache_fwd_params {
+    const void* Q;
+    void* O;
+    int Hq;
+    long long total, q_stride_t, q_stride_h, o_stride_t, o_stride_h;
+    int max_new, causal;
+    float scale;
+    float* lse;
+    void* workspace;
+    size_t workspace_bytes;
+} flat_attn_cache_fwd_params_t;
+int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_params_t* p, void* stream);
+size_t flat_attn_cache_workspace_bytes(int Hq, int Hkv, int d);   /* for the current device; 0 for bad sizes              */
+
+/*
  * The activation-weight operators of an attention layer (paper Section 2, "Computation
  * operators": step 1, the Query / Key / Value projections of the input; step 5, the Output
  * projection of the concatenated heads).  bf16 operands, fp32 accumulation, bf16 results; the

@@ -55,8 +55,12 @@ EXPORTS = ["flat_attn_fwd", "flat_attn_fwd_ex", "flat_attn_naive_fwd", "flat_att
            "flat_qkv_proj_fwd", "flat_out_proj_fwd", "flat_attn_layer_fwd", "flat_fc_fwd",
            "flat_attn_varlen_fwd", "flat_attn_last_variant", "flat_attn_last_device_error",
            "flat_attn_clear_device_error", "flat_attn_bwd", "flat_attn_bwd_ex", "flat_layernorm_fwd",
-           "flat_attn_last_schedule"]
+           "flat_attn_last_schedule", "flat_attn_rope_table", "flat_attn_rope_fwd", "flat_attn_rope_bwd",
+           "flat_attn_cache_append", "flat_attn_cache_fwd", "flat_attn_cache_workspace_bytes"]
 FLAT_SCHEDULE_ITEMS, FLAT_SCHEDULE_PERSISTENT, FLAT_SCHEDULE_EVEN_DEAL = 1, 2, 3
+
+FLAT_ROPE_PLAIN, FLAT_ROPE_LINEAR, FLAT_ROPE_BASE, FLAT_ROPE_PARTS = 0, 1, 2, 3
+FLAT_CACHE_BAD_PAGE, FLAT_CACHE_BAD_LENGTH = 0xB00, 0xB01
 
 
 class flat_attn_params_t(ctypes.Structure):
@@ -77,6 +81,29 @@ class flat_attn_bwd_params_t(ctypes.Structure):
                 ("B", ctypes.c_int), ("H", ctypes.c_int), ("Nq", ctypes.c_int), ("Nk", ctypes.c_int),
                 ("d", ctypes.c_int), ("scale", ctypes.c_float), ("k_valid_len", ctypes.c_void_p),
                 ("status", ctypes.c_void_p), ("causal", ctypes.c_int)]
+
+
+class flat_attn_rope_params_t(ctypes.Structure):
+    _fields_ = [("Q", ctypes.c_void_p), ("K", ctypes.c_void_p), ("Qr", ctypes.c_void_p), ("Kr", ctypes.c_void_p),
+                ("B", ctypes.c_int), ("N", ctypes.c_int), ("Hq", ctypes.c_int), ("Hk", ctypes.c_int), ("d", ctypes.c_int),
+                ("q_stride", ctypes.c_longlong * 3), ("k_stride", ctypes.c_longlong * 3), ("qr_stride", ctypes.c_longlong * 3),
+                ("kr_stride", ctypes.c_longlong * 3), ("positions", ctypes.c_void_p), ("positions_stride_b", ctypes.c_longlong),
+                ("table", ctypes.c_void_p), ("rotary_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("amplitude", ctypes.c_float),
+                ("dtype", ctypes.c_int)]
+
+
+class flat_attn_cache_t(ctypes.Structure):
+    _fields_ = [("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("cu_seqlens", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int), ("d", ctypes.c_int),
+                ("num_seqs", ctypes.c_int), ("max_pages", ctypes.c_int), ("status", ctypes.c_void_p)]
+
+
+class flat_attn_cache_fwd_params_t(ctypes.Structure):
+    _fields_ = [("Q", ctypes.c_void_p), ("O", ctypes.c_void_p), ("Hq", ctypes.c_int), ("total", ctypes.c_longlong),
+                ("q_stride_t", ctypes.c_longlong), ("q_stride_h", ctypes.c_longlong), ("o_stride_t", ctypes.c_longlong),
+                ("o_stride_h", ctypes.c_longlong), ("max_new", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float),
+                ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 _vp, _i, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_float
@@ -115,6 +142,19 @@ _lib.flat_attn_varlen_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, 
 _lib.flat_attn_varlen_fwd.restype = _i
 _lib.flat_attn_host_workspace_bytes.argtypes = [_i, _i, _i, _i, _i, _i]
 _lib.flat_attn_host_workspace_bytes.restype = ctypes.c_size_t
+_ll, _d = ctypes.c_longlong, ctypes.c_double
+_lib.flat_attn_rope_table.argtypes = [_i, _d, _i, _d, _ll, _d, _d, _vp, _vp]
+_lib.flat_attn_rope_table.restype = _i
+_lib.flat_attn_rope_fwd.argtypes = [ctypes.POINTER(flat_attn_rope_params_t), _vp]
+_lib.flat_attn_rope_fwd.restype = _i
+_lib.flat_attn_rope_bwd.argtypes = [ctypes.POINTER(flat_attn_rope_params_t), _vp]
+_lib.flat_attn_rope_bwd.restype = _i
+_lib.flat_attn_cache_append.argtypes = [ctypes.POINTER(flat_attn_cache_t), _vp, _vp, _ll, _ll, _ll, _ll, _ll, _i, _vp]
+_lib.flat_attn_cache_append.restype = _i
+_lib.flat_attn_cache_fwd.argtypes = [ctypes.POINTER(flat_attn_cache_t), ctypes.POINTER(flat_attn_cache_fwd_params_t), _vp]
+_lib.flat_attn_cache_fwd.restype = _i
+_lib.flat_attn_cache_workspace_bytes.argtypes = [_i, _i, _i]
+_lib.flat_attn_cache_workspace_bytes.restype = ctypes.c_size_t
 _lib.flat_attn_last_launch_count.restype = _i
 _lib.flat_attn_last_variant.restype = _i
 _lib.flat_attn_last_schedule.restype = _i
@@ -477,6 +517,167 @@ def flat_attn_varlen_fwd(Q, K, V, O, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, s
     _check(_lib.flat_attn_varlen_fwd(_ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(cu_seqlens_q), _ptr(cu_seqlens_k),
                                      cu_seqlens_q.numel() - 1, H, d, total_q, total_k, int(max_seqlen_q), float(scale),
                                      1 if causal else 0, _ptr(status), _stream_ptr(stream)))
+    return O
+
+
+def flat_attn_rope_table(rotary_dim, base=10000.0, scaling=FLAT_ROPE_PLAIN, factor=1.0, original_len=0, low=1.0, high=32.0, device="cuda"):
+    """The frequencies of rotary positions as the kernels read them (int64 [rotary_dim / 2], units of 2^-64 turns a token) and the
+    amplitude that goes with them.  Made once for a model; scaling: FLAT_ROPE_PLAIN, _LINEAR (angles / factor), _BASE (the base
+    raised) or _PARTS (frequency by frequency, by its turns over original_len)."""
+    words = (ctypes.c_uint64 * max(1, int(rotary_dim) // 2))()
+    amplitude = ctypes.c_float(0.0)
+    _check(_lib.flat_attn_rope_table(int(rotary_dim), float(base), int(scaling), float(factor), int(original_len), float(low), float(high),
+                                     ctypes.addressof(words), ctypes.addressof(amplitude)))
+    table = torch.frombuffer(bytearray(bytes(words)), dtype=torch.int64)
+    return table.to(device), float(amplitude.value)
+
+
+def _here(**tensors):
+    """All on the current device: kernels run there."""
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+            raise ValueError(name + " must be a CUDA tensor on the current device")
+
+
+def _rows_contiguous(name, t, dtype, shape):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError("%s must be a %s tensor of shape %s whose last dimension is contiguous" % (name, dtype, tuple(shape)))
+
+
+def _step(t, dim):
+    return 0 if t.shape[dim] == 1 else t.stride(dim)
+
+
+def _rope(back, Q, K, table, Qr, Kr, positions, interleaved, amplitude, stream):
+    rc = _binding.rope(Q, K, table, Qr, Kr, positions, interleaved, amplitude, back, stream)
+    if rc >= 0:
+        if rc:
+            raise FlatAttnError(rc)
+        return (Qr, Kr) if K is not None else Qr
+    if Q.dim() not in (3, 4):
+        raise ValueError("expected [B, H, N, d] or packed [T, H, d]")
+    if Q.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("Q and K must be bfloat16 or float32")
+    if (K is None) != (Kr is None):
+        raise ValueError("K and its output go together")
+    at = (0, 1, 2) if Q.dim() == 4 else (None, 1, 0)              # batch, head, token
+    B, Hq, N, d = (1 if at[0] is None else Q.shape[0]), Q.shape[1], Q.shape[at[2]], Q.shape[-1]
+    _rows_contiguous("Q", Q, Q.dtype, Q.shape)
+    _rows_contiguous("Qr", Qr, Q.dtype, Q.shape)
+    if K is not None:
+        shape = list(Q.shape)
+        shape[1] = K.shape[1] if K.dim() == Q.dim() else -1
+        _rows_contiguous("K", K, Q.dtype, shape)
+        _rows_contiguous("Kr", Kr, Q.dtype, shape)
+    if table.dtype != torch.int64 or table.dim() != 1 or not table.is_contiguous() or table.numel() > 64:
+        raise ValueError("table must come from flat_attn_rope_table")
+    if positions is not None and (positions.dtype != torch.int32 or not positions.is_contiguous()
+                                  or tuple(positions.shape) not in ((N,), (B, N) if Q.dim() == 4 else (N,))):
+        raise ValueError("positions must be a contiguous int32 tensor [N], or [B, N] for dense tensors")
+    _here(Q=Q, K=K, table=table, Qr=Qr, Kr=Kr, positions=positions)
+    p = flat_attn_rope_params_t()
+    p.Q, p.Qr = Q.data_ptr(), Qr.data_ptr()
+    p.K, p.Kr = (None, None) if K is None else (K.data_ptr(), Kr.data_ptr())
+    p.B, p.N, p.Hq, p.Hk, p.d = B, N, Hq, 0 if K is None else K.shape[1], d
+    for name, t in (("q_stride", Q), ("qr_stride", Qr), ("k_stride", K), ("kr_stride", Kr)):
+        if t is not None:
+            setattr(p, name, (ctypes.c_longlong * 3)(*(0 if i is None else _step(t, i) for i in at)))
+    p.positions = None if positions is None else positions.data_ptr()
+    p.positions_stride_b = N if positions is not None and positions.dim() == 2 else 0
+    p.table, p.rotary_dim = table.data_ptr(), 2 * table.numel()
+    p.interleaved, p.amplitude, p.dtype = 1 if interleaved else 0, float(amplitude), _dtype_code(Q)
+    _check((_lib.flat_attn_rope_bwd if back else _lib.flat_attn_rope_fwd)(ctypes.byref(p), _stream_ptr(stream)))
+    return (Qr, Kr) if K is not None else Qr
+
+
+def flat_attn_rope_fwd(Q, K, table, Qr, Kr, positions=None, interleaved=False, amplitude=1.0, stream=None):
+    """Rotary positions: Qr, Kr = Q, K with the first 2 * table.numel() features of every head rotated by the token's position.
+    Dense [B, H, N, d] or packed [T, H, d] (bf16 or fp32, last dimension contiguous, other strides free; K and Kr may have
+    another number of heads, or be None).  positions: int32 [N] or [B, N] (None: 0 .. N - 1); pairs (i, i + r / 2), or (2 i, 2 i + 1)
+    where interleaved.  Qr may be Q, Kr K.  table and amplitude: flat_attn_rope_table."""
+    return _rope(False, Q, K, table, Qr, Kr, positions, interleaved, amplitude, stream)
+
+
+def flat_attn_rope_bwd(dQr, dKr, table, dQ, dK, positions=None, interleaved=False, amplitude=1.0, stream=None):
+    """The gradient of flat_attn_rope_fwd: dQ, dK from dQr, dKr (the rotation the other way), same arguments."""
+    return _rope(True, dQr, dKr, table, dQ, dK, positions, interleaved, amplitude, stream)
+
+
+def _cache(k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, status):
+    if k_cache.dim() != 4 or seq_lens.dim() != 1 or page_table.dim() != 2:
+        raise ValueError("expected k_cache, v_cache [num_pages, Hkv, page, d], page_table [num_seqs, max_pages], seq_lens [num_seqs]")
+    pages, H, page, d = k_cache.shape
+    seqs = seq_lens.shape[0]
+    for name, t, dtype, shape in (("k_cache", k_cache, torch.float8_e4m3fn, (pages, H, page, d)),
+                                  ("v_cache", v_cache, torch.float8_e4m3fn, (pages, H, page, d)),
+                                  ("k_exp", k_exp, torch.uint8, (pages, H)), ("v_exp", v_exp, torch.uint8, (pages, H)),
+                                  ("page_table", page_table, torch.int32, (seqs, page_table.shape[1])),
+                                  ("cu_seqlens", cu_seqlens, torch.int32, (seqs + 1,)), ("seq_lens", seq_lens, torch.int32, (seqs,))):
+        if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dtype, shape))
+    _here(k_cache=k_cache, v_cache=v_cache, k_exp=k_exp, v_exp=v_exp, page_table=page_table, cu_seqlens=cu_seqlens, seq_lens=seq_lens,
+          status=status)
+    c = flat_attn_cache_t()
+    c.k_cache, c.v_cache, c.k_exp, c.v_exp = k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr()
+    c.page_table, c.cu_seqlens, c.seq_lens = page_table.data_ptr(), cu_seqlens.data_ptr(), seq_lens.data_ptr()
+    c.num_pages, c.Hkv, c.page, c.d, c.num_seqs, c.max_pages = pages, H, page, d, seqs, page_table.shape[1]
+    c.status = None if status is None else status.data_ptr()
+    return c
+
+
+def flat_attn_cache_append(K, V, k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, max_new, status=None, stream=None):
+    """Writes new tokens' K, V [T, Hkv, d] (bf16, last dimension contiguous) to their places in the 8-bit paged cache k_cache, v_cache
+    [num_pages, Hkv, page, d] (float8_e4m3fn) with scales 2^(exp - 127), k_exp, v_exp [num_pages, Hkv] uint8.  Sequence s owns the new
+    tokens cu_seqlens[s] .. cu_seqlens[s + 1] - 1, the last ones of its seq_lens[s] tokens; page_table [num_seqs, max_pages] int32."""
+    rc = _binding.cache_append(K, V, k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, max_new, status, stream)
+    if rc >= 0:
+        if rc:
+            raise FlatAttnError(rc)
+        return k_cache, v_cache
+    c = _cache(k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, status)
+    shape = (K.shape[0], c.Hkv, c.d)
+    _rows_contiguous("K", K, torch.bfloat16, shape)
+    _rows_contiguous("V", V, torch.bfloat16, shape)
+    _here(K=K, V=V)
+    _check(_lib.flat_attn_cache_append(ctypes.byref(c), _ptr(K), _ptr(V), K.shape[0], _step(K, 0), _step(K, 1), _step(V, 0), _step(V, 1),
+                                       int(max_new), _stream_ptr(stream)))
+    return k_cache, v_cache
+
+
+def flat_attn_cache_workspace_bytes(Hq, Hkv, d) -> int:
+    """Bytes of the workspace of flat_attn_cache_fwd on the current device: torch.zeros(bytes, dtype=torch.uint8, device="cuda"), once."""
+    return int(_lib.flat_attn_cache_workspace_bytes(int(Hq), int(Hkv), int(d)))
+
+
+def flat_attn_cache_fwd(Q, O, k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, max_seqlen_q, scale, workspace, causal=False,
+                        lse=None, status=None, stream=None):
+    """Attention of packed queries Q, O [T, Hq, d] (bf16, last dimension contiguous; Hq a multiple of Hkv) over the 8-bit paged cache
+    (flat_attn_cache_append): the queries cu_seqlens[s] .. cu_seqlens[s + 1] - 1 over the seq_lens[s] tokens of sequence s.  causal:
+    they are its last tokens.  One query a sequence, a few, long chunks or any mix.  `workspace`: uint8, zeroed once, one for
+    each stream; lse [T, Hq] float32 is optional."""
+    rc = _binding.cache_fwd(Q, O, k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, max_seqlen_q, scale, workspace, causal,
+                            lse, status, stream)
+    if rc >= 0:
+        if rc:
+            raise FlatAttnError(rc)
+        return O
+    c = _cache(k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, status)
+    if Q.dim() != 3:
+        raise ValueError("expected Q, O [T, Hq, d]")
+    _rows_contiguous("Q", Q, torch.bfloat16, (Q.shape[0], Q.shape[1], c.d))
+    _rows_contiguous("O", O, torch.bfloat16, Q.shape)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != tuple(Q.shape[:2]) or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous float32 tensor [T, Hq]")
+    _here(Q=Q, O=O, workspace=workspace, lse=lse)
+    p = flat_attn_cache_fwd_params_t()
+    p.Q, p.O, p.Hq, p.total = Q.data_ptr(), O.data_ptr(), Q.shape[1], Q.shape[0]
+    p.q_stride_t, p.q_stride_h, p.o_stride_t, p.o_stride_h = _step(Q, 0), _step(Q, 1), _step(O, 0), _step(O, 1)
+    p.max_new, p.causal, p.scale = int(max_seqlen_q), 1 if causal else 0, float(scale)
+    p.lse = None if lse is None else lse.data_ptr()
+    p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(_lib.flat_attn_cache_fwd(ctypes.byref(c), ctypes.byref(p), _stream_ptr(stream)))
     return O
 
 

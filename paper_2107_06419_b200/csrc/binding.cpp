@@ -12,6 +12,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -39,6 +40,26 @@ struct Args {
         return &t;
     }
     const at::Tensor* bf16() { return tensor(at::kBFloat16); }
+    // One of any strides whose last dimension is contiguous, on the current device.
+    const at::Tensor* strided(at::ScalarType type, bool none_ok = false) {
+        PyObject* o = next();
+        if (o == Py_None && none_ok) return nullptr;
+        if (bad || !THPVariable_CheckExact(o)) { bad = true; return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.scalar_type() != type || t.dim() < 2 || (t.size(-1) > 1 && t.stride(-1) != 1) || !here(t)) { bad = true; return nullptr; }
+        return &t;
+    }
+    // A contiguous one on the current device.
+    const at::Tensor* local(at::ScalarType type, bool none_ok = false) {
+        const at::Tensor* t = tensor(type, none_ok);
+        if (t && !here(*t)) { bad = true; return nullptr; }
+        return t;
+    }
+    int device = -1;
+    bool here(const at::Tensor& t) {
+        if (device < 0) device = c10::cuda::current_device();
+        return t.get_device() == device;
+    }
     double number() {
         PyObject* o = next();
         if (PyFloat_CheckExact(o)) return PyFloat_AS_DOUBLE(o);
@@ -297,6 +318,114 @@ PyObject* layernorm_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {   // X
     return run([&] { return flat_layernorm_fwd(x, r, gamma, beta, y, M, static_cast<int>(D), eps, st); });
 }
 
+// The stride of a dimension, 0 where it has one element (torch may report any number there).
+inline long long step(const at::Tensor& t, int dim) { return t.size(dim) == 1 ? 0 : t.stride(dim); }
+
+PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    // Q, K, table, Qr, Kr, positions, interleaved, amplitude, back, stream
+    if (n < 1) return no();
+    Args a{args, n};
+    flat_attn_rope_params_t p{};
+    const at::ScalarType type = type_of(args[0]);
+    if (type != at::kBFloat16 && type != at::kFloat) return no();
+    const at::Tensor *Q = a.strided(type), *K = a.strided(type, true), *table = a.local(at::kLong), *Qr = a.strided(type),
+                     *Kr = a.strided(type, true), *pos = a.local(at::kInt, true);
+    p.interleaved = a.truth();
+    p.amplitude = static_cast<float>(a.number());
+    const int back = a.truth();
+    void* st = a.stream();
+    a.end();
+    if (a.bad || !K != !Kr || table->dim() != 1) return no();
+    const int dims = static_cast<int>(Q->dim());
+    if (dims != 3 && dims != 4) return no();
+    // [B, H, N, d], or packed [T, H, d]
+    const int db = dims == 4 ? 0 : -1, dn = dims == 4 ? 2 : 0, dh = 1;
+    const int64_t B = db < 0 ? 1 : Q->size(db), N = Q->size(dn), Hq = Q->size(dh), d = Q->size(dims - 1), Hk = K ? K->size(dh) : 0;
+    if (!Qr->sizes().equals(Q->sizes()) || (K && (K->dim() != dims || !Kr->sizes().equals(K->sizes()) || K->size(dn) != N ||
+                                                  K->size(dims - 1) != d || (db >= 0 && K->size(db) != B))))
+        return no();
+    if (!small(B) || !small(N) || !small(Hq) || !small(Hk) || !small(d) || !small(table->size(0)) || table->size(0) > 64) return no();
+    if (pos && !is(*pos, {N}) && !(db >= 0 && is(*pos, {B, N}))) return no();
+    auto strides = [&](const at::Tensor& t, long long (&s)[3]) {
+        s[0] = db < 0 ? 0 : step(t, db);
+        s[1] = step(t, dh);
+        s[2] = step(t, dn);
+    };
+    strides(*Q, p.q_stride);
+    strides(*Qr, p.qr_stride);
+    if (K) { strides(*K, p.k_stride); strides(*Kr, p.kr_stride); }
+    p.Q = ptr(Q); p.Qr = ptr(Qr); p.K = ptr(K); p.Kr = ptr(Kr);
+    p.B = static_cast<int>(B); p.N = static_cast<int>(N); p.Hq = static_cast<int>(Hq); p.Hk = static_cast<int>(Hk); p.d = static_cast<int>(d);
+    p.positions = at_<const int32_t>(pos);
+    p.positions_stride_b = pos && pos->dim() == 2 ? N : 0;
+    p.table = at_<const uint64_t>(table);
+    p.rotary_dim = 2 * static_cast<int>(table->size(0));
+    p.dtype = type == at::kFloat ? FLAT_DTYPE_F32 : FLAT_DTYPE_BF16;
+    return run([&] { return back ? flat_attn_rope_bwd(&p, st) : flat_attn_rope_fwd(&p, st); });
+}
+
+// k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens
+bool cache_args(Args& a, flat_attn_cache_t& c) {
+    const at::Tensor *k = a.local(at::kFloat8_e4m3fn), *v = a.local(at::kFloat8_e4m3fn), *ke = a.local(at::kByte), *ve = a.local(at::kByte),
+                     *table = a.local(at::kInt), *cu = a.local(at::kInt), *lens = a.local(at::kInt);
+    if (a.bad || k->dim() != 4 || table->dim() != 2 || lens->dim() != 1) return false;
+    const int64_t pages = k->size(0), H = k->size(1), page = k->size(2), d = k->size(3), seqs = lens->size(0), most = table->size(1);
+    if (!v->sizes().equals(k->sizes()) || !is(*ke, {pages, H}) || !is(*ve, {pages, H}) || !is(*cu, {seqs + 1}) || table->size(0) != seqs ||
+        !small(pages) || !small(H) || !small(page) || !small(d) || !small(seqs) || !small(most))
+        return false;
+    c.k_cache = ptr(k); c.v_cache = ptr(v);
+    c.k_exp = at_<uint8_t>(ke); c.v_exp = at_<uint8_t>(ve);
+    c.page_table = at_<const int32_t>(table); c.cu_seqlens = at_<const int32_t>(cu); c.seq_lens = at_<const int32_t>(lens);
+    c.num_pages = static_cast<int>(pages); c.Hkv = static_cast<int>(H); c.page = static_cast<int>(page); c.d = static_cast<int>(d);
+    c.num_seqs = static_cast<int>(seqs); c.max_pages = static_cast<int>(most);
+    return true;
+}
+
+PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    // K, V, k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, max_new, status, stream
+    Args a{args, n};
+    flat_attn_cache_t c{};
+    const at::Tensor *K = a.strided(at::kBFloat16), *V = a.strided(at::kBFloat16);
+    if (a.bad || !cache_args(a, c)) return no();
+    const int most = a.whole();
+    c.status = a.status();
+    void* st = a.stream();
+    a.end();
+    if (a.bad || K->dim() != 3 || K->size(1) != c.Hkv || K->size(2) != c.d || !V->sizes().equals(K->sizes())) return no();
+    const void *k = ptr(K), *v = ptr(V);
+    const int64_t total = K->size(0);
+    const long long kt = step(*K, 0), kh = step(*K, 1), vt = step(*V, 0), vh = step(*V, 1);
+    return run([&] { return flat_attn_cache_append(&c, k, v, total, kt, kh, vt, vh, most, st); });
+}
+
+PyObject* cache_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    // Q, O, k_cache, v_cache, k_exp, v_exp, page_table, cu_seqlens, seq_lens, max_new, scale, workspace, causal, lse, status, stream
+    Args a{args, n};
+    flat_attn_cache_t c{};
+    flat_attn_cache_fwd_params_t p{};
+    const at::Tensor *Q = a.strided(at::kBFloat16), *O = a.strided(at::kBFloat16);
+    if (a.bad || !cache_args(a, c)) return no();
+    p.max_new = a.whole();
+    p.scale = static_cast<float>(a.number());
+    const at::Tensor* work = a.local(at::kByte);
+    p.causal = a.truth();
+    const at::Tensor* lse = a.local(at::kFloat, true);
+    c.status = a.status();
+    void* st = a.stream();
+    a.end();
+    if (a.bad || Q->dim() != 3 || Q->size(2) != c.d || !small(Q->size(1)) || !O->sizes().equals(Q->sizes()) ||
+        (lse && !is(*lse, {Q->size(0), Q->size(1)})))
+        return no();
+    p.Q = ptr(Q); p.O = ptr(O);
+    p.Hq = static_cast<int>(Q->size(1));
+    p.total = Q->size(0);
+    p.q_stride_t = step(*Q, 0); p.q_stride_h = step(*Q, 1); p.o_stride_t = step(*O, 0); p.o_stride_h = step(*O, 1);
+    p.lse = at_<float>(lse);
+    p.workspace = ptr(work);
+    p.workspace_bytes = static_cast<size_t>(work->numel());
+    return run([&] { return flat_attn_cache_fwd(&c, &p, st); });
+}
+
 // The functions as Python sees them: no C++ exception leaves them.
 typedef PyObject* Fast(PyObject*, PyObject* const*, Py_ssize_t);
 template <Fast* F> PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -310,7 +439,7 @@ template <Fast* F> PyObject* guarded(PyObject* self, PyObject* const* args, Py_s
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<f>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(fwd), FAST(fwd_ex), FAST(bwd), FAST(bwd_ex), FAST(varlen_fwd), FAST(layer_fwd), FAST(fc_fwd),
-                         FAST(layernorm_fwd), {nullptr, nullptr, 0, nullptr}};
+                         FAST(layernorm_fwd), FAST(rope), FAST(cache_append), FAST(cache_fwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,582 @@
+// Attention over the 8-bit paged cache, for few query rows per key head: decode steps and drafts (d = 64 and 128).
+//
+// With K = 2^ek k and V = 2^ev v (k, v: e4m3; one ek, ev a page and head), a row's output is sum_j w_j 2^ev_j v_j / sum_j w_j,
+// w_j = 2^(x_j - m), x_j = (q . k_j) scale log2(e) 2^ek_j.  e4m3 numbers are exact in half precision, so they go into the warp-level
+// m16n8k16 products (half in, fp32 out) as they are; the scale of the keys is one multiplication per sixteen logits' constant,
+// the scale of the values is taken relative to the largest one so far and multiplied to the weights before they are rounded.
+// Weights are kept as 2^15 w, which uses half precision's range: what is rounded away lies 2^39 below a row's largest weight.
+//
+// What bounds it: device memory, 2 d bytes a token and key head against 4 d FLOP a query row.  The rows of a unit are the queries
+// of one sequence times the G query heads that share a key head, sixteen to a tile, so the cache is read once for up to sixteen rows.
+// Work is dealt by chunks of 8 KB (keys and values of 32 tokens, d = 128): all chunks of all (sequence, key head, row tile) in one
+// row, an equal share of neighbouring chunks to each team.  A team is a CTA (four warps, which take a part's chunks in turn
+// and join through shared memory), or one warp where there are more items than warps.  An item that ends up in several teams
+// is joined by whichever of them comes last, from their normalised outputs and log-sums, in the order of the keys.
+// Every warp keeps its own ring of three chunks (cp.async, 16 bytes a lane and instruction: any page size and order, tokens behind the
+// length filled with zeros), so no barrier is in the loop.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "cache_common.cuh"
+#include "flat_internal.cuh"
+#include "ptx_sm100.cuh"
+#include "tc_common.cuh"
+
+namespace flat {
+
+using namespace cache;
+
+namespace {
+
+constexpr int WARPS = 4, THREADS = 32 * WARPS, STAGES = 3, CTAS = 2;      // (CTAS: per SM)
+constexpr int HALF_BYTES = 4096, CHUNK_BYTES = 2 * HALF_BYTES;            // a chunk's keys, then its values
+constexpr int SMEM_BYTES = WARPS * STAGES * CHUNK_BYTES;
+constexpr float WEIGHT_SHIFT = 15.f;                                      // weights are kept as 2^15 w
+
+struct DecodeArgs {
+    CacheView c;
+    const __nv_bfloat16* Q;
+    __nv_bfloat16* O;
+    float* lse;
+    long long q_st, q_sh, o_st, o_sh, total;
+    int Hq, G, max_new, most_rows, causal;               // sequences with more than most_rows rows are not this kernel's
+    float scale_log2e;
+    int* counters;                                       // [teams], 0 between launches
+    float* part_lse;                                     // [2 teams][16], base 2
+    float* part_o;                                       // [2 teams][16][D]
+};
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool take) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_groups() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void lds16(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// c (16 x 8) += a (16 x 16) b (16 x 8), half precision in
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two e4m3 (the lower or upper half of a word) as two half-precision numbers.
+__device__ __forceinline__ uint32_t halves(uint32_t two) {
+    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
+    return static_cast<uint32_t>(r.x) | static_cast<uint32_t>(r.y) << 16;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float quad_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    v += __shfl_xor_sync(0xffffffffu, v, 1);
+    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+}
+__device__ __forceinline__ float two_to(int e) {         // 2^e for any e: 0 below, the largest power above
+    e = e < -127 ? -127 : e > 127 ? 127 : e;
+    return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+}
+
+// TEAM: warps of a team (4 or 1).  RG: row groups of eight in a tile (1: no sequence has more than eight rows).
+template <int D, int RG, int TEAM>
+__global__ void __launch_bounds__(THREADS, CTAS)
+cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
+    constexpr int CH = HALF_BYTES / D;                   // tokens of a chunk: 32 (d = 128) or 64
+    constexpr int PIECES = D / 16, RPI = 32 / PIECES;    // 16-byte pieces of a row; rows that a copy instruction brings
+    constexpr int NT = CH / 8;                           // logit blocks of eight keys
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ int ids[WARPS][STAGES][4];                // the chunk's pages; -1: none there
+    __shared__ long long prefix[THREADS + 1];
+    __shared__ float warp_lse[WARPS][16];
+    __shared__ int last_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int member = TEAM == 1 ? 0 : warp;             // the warp's place in its team
+    const int team = TEAM == 1 ? blockIdx.x * WARPS + warp : blockIdx.x, teams = TEAM == 1 ? gridDim.x * WARPS : gridDim.x;
+    const CacheView& cv = p.c;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    // ---------------------------------------------------------------- the deal
+    auto shape = [&](int s, Span& sp, int& nch, int& tiles) -> long long {      // chunks of all items of a sequence
+        nch = tiles = 0;
+        if (!read_span(cv, s, p.total, p.max_new, sp) || sp.n == 0) return 0;
+        const long long rows = static_cast<long long>(sp.n) * p.G;
+        if (rows > p.most_rows) return 0;
+        tiles = static_cast<int>((rows + 15) / 16);
+        nch = (sp.len + CH - 1) / CH;
+        return static_cast<long long>(nch) * tiles * cv.Hkv;
+    };
+    const int per = (cv.num_seqs + THREADS - 1) / THREADS;
+    {
+        long long sum = 0;
+        for (int i = 0; i < per; ++i) {
+            const int s = threadIdx.x * per + i;
+            Span sp;
+            int a, b;
+            if (s < cv.num_seqs) sum += shape(s, sp, a, b);
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        prefix[threadIdx.x + 1] = sum;
+        if (threadIdx.x == 0) prefix[0] = 0;
+        __syncthreads();
+        long long before = 0;
+        for (int w = 0; w < warp; ++w) before += prefix[32 * (w + 1)];
+        __syncthreads();
+        prefix[threadIdx.x + 1] = sum + before;
+        __syncthreads();
+    }
+    const long long all = prefix[THREADS];
+    // an equal share each, of at least two chunks a warp
+    long long share = (all + teams - 1) / teams;
+    if (share < 2 * TEAM) share = 2 * TEAM;
+    long long pos = team * share;
+    const long long begin = pos, end = pos + share < all ? pos + share : all;
+    if (TEAM > 1 && pos >= end) return;                  // (the whole CTA)
+    int s = 0, nch = 0, tiles = 0;
+    Span sp{};
+    long long base = 0, chunks = 0;
+    if (pos < end) {
+        int lo = 0, hi = THREADS;                        // the last thread whose sequences begin at or before pos
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (prefix[mid] <= pos) lo = mid; else hi = mid;
+        }
+        s = lo * per;
+        base = prefix[lo];
+        chunks = shape(s, sp, nch, tiles);
+    }
+
+    const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * CHUNK_BYTES;
+    const int page_mask = cv.page - 1, slots = CH >> cv.page_shift > 0 ? CH >> cv.page_shift : 1;
+    // ldmatrix row of the lane: blocks (keys 0-7, piece x), (8-15, x), (0-7, x + 1), (8-15, x + 1)
+    const int vrow = (lane & 7) + ((lane >> 3) & 1) * 8, vpiece = lane >> 4;
+
+    while (pos < end) {
+        while (pos >= base + chunks) { base += chunks; ++s; chunks = shape(s, sp, nch, tiles); }
+        const long long rel = pos - base, item = rel / nch;
+        const int a0 = static_cast<int>(rel - item * nch);
+        const int a1 = end - pos < nch - a0 ? a0 + static_cast<int>(end - pos) : nch;
+        const int h = static_cast<int>(item / tiles), tile = static_cast<int>(item - static_cast<long long>(h) * tiles);
+        const int rows_left = sp.n * p.G - tile * 16, rows = rows_left < 16 ? rows_left : 16;
+        const long long item_begin = base + item * nch;
+
+        // ------------------------------------------------------------ copies
+        const int count = a1 - a0 - member <= 0 ? 0 : (a1 - a0 - member + TEAM - 1) / TEAM;     // this warp's chunks
+        const int pages = (sp.len + page_mask) >> cv.page_shift;
+        auto load_id = [&](int k) {                      // lane j: the page of the k-th chunk's j-th slot
+            const int chunk = a0 + member + k * TEAM, index = (chunk * CH >> cv.page_shift) + lane;
+            int id = -1;
+            if (k < count && lane < slots && index < pages && !read_page(cv, s, index, id)) id = -1;
+            return id;
+        };
+        auto issue = [&](int k, int id) {
+            if (k < count) {
+                const int st = k % STAGES, key0 = (a0 + member + k * TEAM) * CH;
+                if (lane < 4) ids[warp][st][lane] = id;
+                const long long off = ((static_cast<long long>(id < 0 ? 0 : id) * cv.Hkv + h) << cv.page_shift) * D;
+                const uint32_t dst = ring + st * CHUNK_BYTES;
+#pragma unroll
+                for (int i = 0; i < CH / RPI; ++i) {
+                    const int slot = (i * RPI) >> cv.page_shift, row = i * RPI + lane / PIECES, piece = lane % PIECES;
+                    const long long o = __shfl_sync(0xffffffffu, off, slot);
+                    const bool take = __shfl_sync(0xffffffffu, id, slot) >= 0 && key0 + row < sp.len;
+                    const long long src = o + ((key0 + row) & page_mask) * D + piece * 16;
+                    // (keys: pieces of odd rows change places by four; values: by the row, so that ldmatrix meets eight different banks)
+                    const int kp = D == 128 ? piece ^ ((row & 1) << 2) : piece, vp = D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3);
+                    copy16(dst + row * D + kp * 16, cv.k + src, take);
+                    copy16(dst + HALF_BYTES + row * D + vp * 16, cv.v + src, take);
+                }
+            }
+            commit();
+        };
+        auto load_exps = [&](int k, int& ek, int& ev) {  // lane j: of the k-th chunk's j-th slot
+            ek = ev = 0;
+            if (k < count && lane < slots) {
+                const int id = ids[warp][k % STAGES][lane];
+                if (id >= 0) {
+                    const long long at = static_cast<long long>(id) * cv.Hkv + h;
+                    ek = cv.k_exp[at];
+                    ev = cv.v_exp[at];
+                }
+            }
+        };
+        {
+            int id = load_id(0);
+#pragma unroll
+            for (int k = 0; k < STAGES - 1; ++k) {
+                const int next = load_id(k + 1);
+                issue(k, id);
+                id = next;
+            }
+        }
+        int id_next = load_id(STAGES - 1);
+        __syncwarp();
+        int ek_next, ev_next;
+        load_exps(0, ek_next, ev_next);
+
+        // ------------------------------------------------------------ queries: half precision, a power of two taken out of each row
+        // Slice (x, w) of the contraction: a lane's features 16 (t + 4 x) + 4 w .. + 3, the ones that it reads of a key
+        uint32_t qa[D / 16][4];
+        float unit[RG];
+        int nrow[RG];
+        {
+            uint4 raw[RG][D / 64][2];
+#pragma unroll
+            for (int r = 0; r < RG; ++r) {
+                const int row = g + 8 * r;
+                float top = 0.f;
+                const int flat_row = tile * 16 + row, tok = flat_row / p.G, gh = flat_row - tok * p.G;
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        raw[r][x][e] = make_uint4(0, 0, 0, 0);
+                        if (row < rows)
+                            raw[r][x][e] = reinterpret_cast<const uint4*>(p.Q + (sp.q0 + tok) * p.q_st + (static_cast<long long>(h) * p.G + gh) * p.q_sh + 16 * (t + 4 * x))[e];
+                        const uint32_t w[4] = {raw[r][x][e].x, raw[r][x][e].y, raw[r][x][e].z, raw[r][x][e].w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+                    }
+                top = quad_max(top);
+                int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;      // the row's largest: 2^e to 2^(e + 1)
+                e = e < -100 ? -100 : e;
+                const float up = two_to(14 - e);
+                unit[r] = p.scale_log2e * two_to(e - 14);
+                const long long lim = static_cast<long long>(tok) + 1 + sp.len - sp.n;
+                nrow[r] = row < rows ? (p.causal && lim < sp.len ? static_cast<int>(lim) : sp.len) : 0;
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint4& v = raw[r][x][w >> 1];
+                        const uint32_t lo = w & 1 ? v.z : v.x, hi = w & 1 ? v.w : v.y;
+                        qa[4 * x + w][r] = pack_half2(__uint_as_float(lo << 16) * up, __uint_as_float(lo & 0xffff0000u) * up);
+                        qa[4 * x + w][2 + r] = pack_half2(__uint_as_float(hi << 16) * up, __uint_as_float(hi & 0xffff0000u) * up);
+                        if (RG == 1) qa[4 * x + w][1] = qa[4 * x + w][3] = 0u;
+                    }
+            }
+        }
+        const long long lim0 = static_cast<long long>(tile * 16 / p.G) + 1 + sp.len - sp.n;     // keys that every row sees
+        const int nmin = p.causal && lim0 < sp.len ? static_cast<int>(lim0) : sp.len;
+
+        // ------------------------------------------------------------ the chunks
+        float o[D / 8][4], m[RG], l[RG];
+        int E = -1000;                                   // o is in units of 2^E
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+#pragma unroll
+        for (int r = 0; r < RG; ++r) { m[r] = -INFINITY; l[r] = 0.f; }
+        for (int k = 0; k < count; ++k) {
+            const int st = k % STAGES, key0 = (a0 + member + k * TEAM) * CH;
+            wait_groups<STAGES - 2>();
+            __syncwarp();
+            const int ek = ek_next, ev = ev_next;
+            // bit j: slot j has no page
+            const int bad = __ballot_sync(0xffffffffu, lane < slots && ids[warp][st][lane & 3] < 0);
+            issue(k + STAGES - 1, id_next);              // (into the stage that every lane had read before this chunk's barrier)
+            id_next = load_id(k + STAGES);
+            const uint32_t ks = ring + st * CHUNK_BYTES, vs = ks + HALF_BYTES;
+            float c[NT][4];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c[i][e] = 0.f;
+                const int row = i * 8 + g;
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x) {
+                    uint32_t w[4];
+                    lds16(ks + row * D + (D == 128 ? (t + 4 * x) ^ ((row & 1) << 2) : t) * 16, w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mma16(c[i], qa[4 * x + e], halves(w[e] & 0xffffu), halves(w[e] >> 16));
+                }
+            }
+            // base-2 logits; keys that a row does not see take no part
+            const bool masked = key0 + CH > nmin || bad != 0;
+            float mx[RG], wv[NT / 2];                    // wv: what the weights of sixteen keys are multiplied by for their values' scale
+            int e_top = -1000;
+#pragma unroll
+            for (int i = 0; i < NT / 2; ++i) {
+                const int v = __shfl_sync(0xffffffffu, ev, (i * 16) >> cv.page_shift);
+                wv[i] = __int_as_float(v);
+                if (v > e_top) e_top = v;
+            }
+            bool grown = false;
+            if (e_top > E) {
+                const float down = E < -500 ? 0.f : two_to(E - e_top);
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[i][e] *= down;
+                E = e_top;
+            }
+#pragma unroll
+            for (int i = 0; i < NT / 2; ++i) wv[i] = two_to(__float_as_int(wv[i]) - E);
+#pragma unroll
+            for (int r = 0; r < RG; ++r) {
+                mx[r] = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const int slot = (i * 8) >> cv.page_shift;
+                    const float u = unit[r] * two_to(__shfl_sync(0xffffffffu, ek, slot) - 127);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float x = c[i][2 * r + e] * u;
+                        if (masked && (key0 + i * 8 + 2 * t + e >= nrow[r] || (bad >> slot & 1))) x = -INFINITY;
+                        c[i][2 * r + e] = x;
+                        mx[r] = fmaxf(mx[r], x);
+                    }
+                }
+                mx[r] = quad_max(mx[r]);
+                grown = grown || mx[r] > m[r];
+            }
+            if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+                for (int r = 0; r < RG; ++r) {
+                    const float mn = fmaxf(m[r], mx[r]);
+                    const float a = mn == -INFINITY ? 1.f : tc::ex2_approx(m[r] - mn);
+                    m[r] = mn;
+                    l[r] *= a;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) { o[i][2 * r] *= a; o[i][2 * r + 1] *= a; }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < RG; ++r) {
+                const float ref = m[r] == -INFINITY ? 0.f : m[r] - WEIGHT_SHIFT;
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float w = tc::ex2_approx(c[i][2 * r + e] - ref);
+                        l[r] += w;
+                        c[i][2 * r + e] = w * wv[i / 2];
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < NT; i += 2) {
+                const uint32_t pa[4] = {pack_half2(c[i][0], c[i][1]), RG == 2 ? pack_half2(c[i][2], c[i][3]) : 0u,
+                                        pack_half2(c[i + 1][0], c[i + 1][1]), RG == 2 ? pack_half2(c[i + 1][2], c[i + 1][3]) : 0u};
+                const int row = i * 8 + vrow;
+#pragma unroll
+                for (int x = 0; x < PIECES; x += 2) {
+                    const int piece = x + vpiece;
+                    uint32_t b[4];
+                    ldsm4_t(vs + row * D + (D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3)) * 16, b);
+                    // a word: features 2 g, 2 g + 1 of key 2 t, then of key 2 t + 1
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint32_t lo = __byte_perm(b[2 * y], 0, 0x3120), hi = __byte_perm(b[2 * y + 1], 0, 0x3120);
+                        mma16(o[2 * (x + y)], pa, halves(lo & 0xffffu), halves(hi & 0xffffu));
+                        mma16(o[2 * (x + y) + 1], pa, halves(lo >> 16), halves(hi >> 16));
+                    }
+                }
+            }
+            load_exps(k + 1, ek_next, ev_next);
+        }
+        wait_groups<0>();
+
+        // ------------------------------------------------------------ normalised outputs and log-sums of this warp's keys
+        // o[2 x], o[2 x + 1] of row r: features 16 x + 4 t + {0, 2}, {1, 3}
+        float lg[RG];
+#pragma unroll
+        for (int r = 0; r < RG; ++r) {
+            l[r] = quad_sum(l[r]);
+            const float inv = l[r] > 0.f ? two_to(E - 127) / l[r] : l[r] == l[r] ? 0.f : l[r];
+            lg[r] = l[r] > 0.f ? m[r] - WEIGHT_SHIFT + log2f(l[r]) : l[r] == l[r] ? -INFINITY : l[r];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) { o[i][2 * r] *= inv; o[i][2 * r + 1] *= inv; }
+        }
+        const bool whole = a0 == 0 && a1 == nch;
+        const long long first_team = item_begin / share, last_team = (item_begin + nch - 1) / share;
+        const long long slot = 2 * team + (pos == begin ? 0 : 1);
+        auto finish = [&](int row, int col, float4 v, float lse2) {     // four features of the item's row
+            const int flat_row = tile * 16 + row, tok = flat_row / p.G, gh = flat_row - tok * p.G, head = h * p.G + gh;
+            uint2 w;
+            w.x = tc::pack_bf16x2(v.x, v.y);
+            w.y = tc::pack_bf16x2(v.z, v.w);
+            *reinterpret_cast<uint2*>(p.O + (sp.q0 + tok) * p.o_st + head * p.o_sh + col) = w;
+            if (p.lse && col == 0) p.lse[static_cast<long long>(sp.q0 + tok) * p.Hq + head] = lse2 * 0.6931471805599453f;
+        };
+        if (TEAM == 1) {
+#pragma unroll
+            for (int r = 0; r < RG; ++r) {
+                const int row = g + 8 * r;
+                if (row >= rows) continue;
+#pragma unroll
+                for (int x = 0; x < PIECES; ++x) {
+                    const float4 v = make_float4(o[2 * x][2 * r], o[2 * x + 1][2 * r], o[2 * x][2 * r + 1], o[2 * x + 1][2 * r + 1]);
+                    if (whole) finish(row, 16 * x + 4 * t, v, lg[r]);
+                    else *reinterpret_cast<float4*>(p.part_o + (slot * 16 + row) * D + 16 * x + 4 * t) = v;
+                }
+                if (!whole && t == 0) p.part_lse[slot * 16 + row] = lg[r];
+            }
+        } else {
+            // the team's warps join through the memory of their rings
+            __syncthreads();
+            float* parts = reinterpret_cast<float*>(smem);                // [warp][row][D]
+#pragma unroll
+            for (int r = 0; r < RG; ++r) {
+                const int row = g + 8 * r;
+#pragma unroll
+                for (int x = 0; x < PIECES; ++x)
+                    *reinterpret_cast<float4*>(parts + (warp * 16 + row) * D + 16 * x + 4 * t) =
+                        make_float4(o[2 * x][2 * r], o[2 * x + 1][2 * r], o[2 * x][2 * r + 1], o[2 * x + 1][2 * r + 1]);
+                if (t == 0) warp_lse[warp][row] = lg[r];
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
+                const int row = i / (D / 4), col = i % (D / 4) * 4;
+                float top = -INFINITY, sum = 0.f;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w) top = fmaxf(top, warp_lse[w][row]);
+                const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w) {
+                    const float a = tc::ex2_approx(warp_lse[w][row] - ref);
+                    const float4 x = *reinterpret_cast<const float4*>(parts + (w * 16 + row) * D + col);
+                    sum += a;
+                    v.x += a * x.x; v.y += a * x.y; v.z += a * x.z; v.w += a * x.w;
+                }
+                const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum, lse2 = sum > 0.f ? ref + log2f(sum) : sum == sum ? -INFINITY : sum;
+                v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
+                if (whole) finish(row, col, v, lse2);
+                else {
+                    *reinterpret_cast<float4*>(p.part_o + (slot * 16 + row) * D + col) = v;
+                    if (col == 0) p.part_lse[slot * 16 + row] = lse2;
+                }
+            }
+        }
+        // ------------------------------------------------------------ an item in several teams: the last one joins its parts
+        if (!whole) {
+            __threadfence();
+            bool mine;
+            const int parts = static_cast<int>(last_team - first_team) + 1;
+            if (TEAM == 1) {
+                __syncwarp();
+                int old = 0;
+                if (lane == 0) old = atomicAdd(p.counters + first_team, 1);
+                mine = __shfl_sync(0xffffffffu, old, 0) == parts - 1;
+            } else {
+                __syncthreads();
+                if (threadIdx.x == 0) last_word = atomicAdd(p.counters + first_team, 1) == parts - 1;
+                __syncthreads();
+                mine = last_word;
+            }
+            if (mine) {
+                __threadfence();
+                const long long slot0 = 2 * first_team + (item_begin == first_team * share ? 0 : 1);
+                for (int i = TEAM == 1 ? lane : threadIdx.x; i < rows * (D / 4); i += 32 * TEAM) {
+                    const int row = i / (D / 4), col = i % (D / 4) * 4;
+                    float ref = -INFINITY, sum = 0.f;
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                    constexpr int BATCH = 8;
+                    for (int j0 = 0; j0 < parts; j0 += BATCH) {
+                        float lj[BATCH];
+                        float4 x[BATCH];
+                        float top = ref;
+#pragma unroll
+                        for (int j = 0; j < BATCH; ++j) {
+                            lj[j] = -INFINITY;
+                            x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (j0 + j < parts) {
+                                const long long q = j0 + j == 0 ? slot0 : 2 * (first_team + j0 + j);
+                                lj[j] = __ldcg(p.part_lse + q * 16 + row);
+                                x[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + (q * 16 + row) * D + col));
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < BATCH; ++j) top = fmaxf(top, lj[j]);
+                        const float use = top == -INFINITY ? 0.f : top;
+                        const float a0_ = tc::ex2_approx(ref - use);
+                        ref = top;
+                        sum *= a0_;
+                        v.x *= a0_; v.y *= a0_; v.z *= a0_; v.w *= a0_;
+#pragma unroll
+                        for (int j = 0; j < BATCH; ++j) {
+                            const float a = tc::ex2_approx(lj[j] - use);
+                            sum += a;
+                            v.x += a * x[j].x; v.y += a * x[j].y; v.z += a * x[j].z; v.w += a * x[j].w;
+                        }
+                    }
+                    const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
+                    v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
+                    finish(row, col, v, sum > 0.f ? (ref == -INFINITY ? 0.f : ref) + log2f(sum) : sum == sum ? -INFINITY : sum);
+                }
+                if (TEAM == 1 ? lane == 0 : threadIdx.x == 0) p.counters[first_team] = 0;
+            }
+        }
+        if (TEAM > 1) __syncthreads();                   // (the rings' memory is free again)
+        pos += a1 - a0;
+    }
+}
+
+}  // namespace
+
+size_t cache_workspace_bytes(int d) {
+    const size_t teams = static_cast<size_t>(device_sm_count()) * CTAS * WARPS;
+    const size_t counters = (teams * sizeof(int) + 255) & ~size_t(255);
+    return counters + 2 * teams * 16 * sizeof(float) + 2 * teams * 16 * d * sizeof(float);
+}
+
+int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int most_rows, cudaStream_t st) {
+    const int sms = device_sm_count();
+    const size_t teams = static_cast<size_t>(sms) * CTAS * WARPS;
+    DecodeArgs p{};
+    p.c = cache_view(c);
+    p.Q = static_cast<const __nv_bfloat16*>(q.Q);
+    p.O = static_cast<__nv_bfloat16*>(q.O);
+    p.lse = q.lse;
+    p.q_st = q.q_stride_t; p.q_sh = q.q_stride_h; p.o_st = q.o_stride_t; p.o_sh = q.o_stride_h;
+    p.total = q.total;
+    p.Hq = q.Hq; p.G = q.Hq / c.Hkv; p.max_new = q.max_new; p.most_rows = most_rows; p.causal = q.causal;
+    p.scale_log2e = q.scale * 1.4426950408889634f;
+    char* w = static_cast<char*>(q.workspace);
+    p.counters = reinterpret_cast<int*>(w);
+    p.part_lse = reinterpret_cast<float*>(w + ((teams * sizeof(int) + 255) & ~size_t(255)));
+    p.part_o = p.part_lse + 2 * teams * 16;
+    const int64_t rows = static_cast<int64_t>(q.max_new) * p.G, least = rows < most_rows ? rows : most_rows;
+    const int64_t items = static_cast<int64_t>(c.num_seqs) * c.Hkv * ((least + 15) / 16);
+    const bool by_warp = items >= static_cast<int64_t>(teams);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(sms * CTAS);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM_BYTES;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    auto go = [&](auto kernel_ok, void (*kern)(DecodeArgs)) {
+        if (!kernel_ok) return static_cast<int>(FLAT_ERR_CUDA);
+        return static_cast<int>(cudaLaunchKernelEx(&cfg, kern, p) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA);
+    };
+#define FLAT_DECODE(DD, RG, TEAM) go(ensure_dynamic_smem<cache_decode_kernel<DD, RG, TEAM>>(SMEM_BYTES), cache_decode_kernel<DD, RG, TEAM>)
+    if (c.d == 64) {
+        if (rows <= 8) return by_warp ? FLAT_DECODE(64, 1, 1) : FLAT_DECODE(64, 1, 4);
+        return by_warp ? FLAT_DECODE(64, 2, 1) : FLAT_DECODE(64, 2, 4);
+    }
+    if (rows <= 8) return by_warp ? FLAT_DECODE(128, 1, 1) : FLAT_DECODE(128, 1, 4);
+    return by_warp ? FLAT_DECODE(128, 2, 1) : FLAT_DECODE(128, 2, 4);
+#undef FLAT_DECODE
+}
+
+}  // namespace flat

@@ -73,6 +73,63 @@ int validate(const flat_attn_params_t* p, flat::Problem* out) {
     return FLAT_OK;
 }
 
+inline bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// Strides in elements: not negative, multiples of `unit`.
+bool strides_ok(const long long* s, int n, long long unit) {
+    for (int i = 0; i < n; ++i)
+        if (s[i] < 0 || s[i] % unit != 0) return false;
+    return true;
+}
+// What is written must not overlap itself: taken from the innermost stride on, every stride steps over all that lies below it.
+bool apart(const long long* stride, const long long* size, int n, long long row) {
+    bool used[4] = {};
+    long long extent = row;
+    for (int k = 0; k < n; ++k) {
+        int at = -1;
+        for (int i = 0; i < n; ++i)
+            if (!used[i] && (at < 0 || stride[i] < stride[at])) at = i;
+        used[at] = true;
+        if (size[at] > 1) {
+            if (stride[at] < extent) return false;
+            if (stride[at] > INT64_MAX / 16 / size[at]) return false;
+            extent += stride[at] * (size[at] - 1);
+        }
+    }
+    return true;
+}
+
+int validate_rope(const flat_attn_rope_params_t* p) {
+    if (!p || !p->Q || !p->Qr || !p->table || !p->K != !p->Kr) return FLAT_ERR_NULL;
+    if (p->B < 1 || p->N < 1 || p->Hq < 1 || (p->K && p->Hk < 1) || !isfinite(p->amplitude)) return FLAT_ERR_SHAPE;
+    if (p->B > 65535 || static_cast<int64_t>(p->B) * p->N > 0x7fffffff || static_cast<int64_t>(p->Hq) + (p->K ? p->Hk : 0) > 65535) return FLAT_ERR_SHAPE;
+    if (p->dtype != FLAT_DTYPE_BF16 && p->dtype != FLAT_DTYPE_F32) return FLAT_ERR_UNSUPPORTED;
+    if (p->d != 16 && p->d != 32 && p->d != 64 && p->d != 128) return FLAT_ERR_UNSUPPORTED;
+    if (p->rotary_dim < 2 || p->rotary_dim > p->d || p->rotary_dim % 2 != 0) return FLAT_ERR_UNSUPPORTED;
+    if (p->interleaved != 0 && p->interleaved != 1) return FLAT_ERR_UNSUPPORTED;
+    if (!aligned(p->Q, 16) || !aligned(p->Qr, 16) || !aligned(p->K, 16) || !aligned(p->Kr, 16) || !aligned(p->positions, 4) || !aligned(p->table, 8))
+        return FLAT_ERR_ALIGN;
+    const long long unit = p->dtype == FLAT_DTYPE_F32 ? 4 : 8;
+    if (!strides_ok(p->q_stride, 3, unit) || !strides_ok(p->qr_stride, 3, unit) || p->positions_stride_b < 0) return FLAT_ERR_SHAPE;
+    const long long q[3] = {p->B, p->Hq, p->N}, k[3] = {p->B, p->Hk, p->N};
+    if (!apart(p->qr_stride, q, 3, p->d)) return FLAT_ERR_SHAPE;
+    if (p->K && (!strides_ok(p->k_stride, 3, unit) || !strides_ok(p->kr_stride, 3, unit) || !apart(p->kr_stride, k, 3, p->d))) return FLAT_ERR_SHAPE;
+    return FLAT_OK;
+}
+
+// The cache and its tables (what they hold is checked on the device).
+int validate_cache(const flat_attn_cache_t* c) {
+    if (!c || !c->k_cache || !c->v_cache || !c->k_exp || !c->v_exp || !c->page_table || !c->cu_seqlens || !c->seq_lens) return FLAT_ERR_NULL;
+    if (c->num_pages < 1 || c->Hkv < 1 || c->num_seqs < 1 || c->max_pages < 1) return FLAT_ERR_SHAPE;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return FLAT_ERR_UNSUPPORTED;
+    if (c->d != 64 && c->d != 128) return FLAT_ERR_UNSUPPORTED;
+    if (c->Hkv > 65535 || static_cast<int64_t>(c->max_pages) * c->page > (1 << 30)) return FLAT_ERR_SHAPE;
+    if (!aligned(c->k_cache, 16) || !aligned(c->v_cache, 16) || !aligned(c->page_table, 4) || !aligned(c->cu_seqlens, 4) || !aligned(c->seq_lens, 4) ||
+        !aligned(c->status, 4))
+        return FLAT_ERR_ALIGN;
+    return FLAT_OK;
+}
+
 }  // namespace
 
 namespace flat {
@@ -500,6 +557,80 @@ int flat_attn_layer_fwd(const void* X, const void* Wqkv, const void* Wo, void* Y
     rc = flat::launch_out_proj(O, Wo, Y, B, N, H, d, Dm, status_or_library_word(status), st);
     if (rc == FLAT_OK) g_last_launches = 3;
     return rc;
+}
+
+int flat_attn_rope_table(int rotary_dim, double base, int scaling, double factor, long long original_len, double low, double high,
+                         uint64_t* table, float* amplitude) {
+    if (!table || !amplitude) return FLAT_ERR_NULL;
+    if (rotary_dim < 2 || rotary_dim > 128 || rotary_dim % 2 != 0) return FLAT_ERR_UNSUPPORTED;
+    if (scaling < FLAT_ROPE_PLAIN || scaling > FLAT_ROPE_PARTS) return FLAT_ERR_UNSUPPORTED;
+    if (!(base > 1) || !(base <= 1e30) || !(factor >= 1) || !(factor <= 1e6)) return FLAT_ERR_SHAPE;
+    if (scaling == FLAT_ROPE_PARTS && (original_len < 1 || !(low >= 0) || !(high > low) || !isfinite(high))) return FLAT_ERR_SHAPE;
+    // (long double: 64 bits of mantissa, so that a frequency's last bit of 2^-64 turns is the rounding's)
+    constexpr long double TWO_PI = 6.283185307179586476925286766559L;
+    const long double f0 = factor, r = rotary_dim;
+    long double b = base;
+    if (scaling == FLAT_ROPE_BASE && rotary_dim > 2) b *= powl(f0, r / (r - 2));
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        long double f = powl(b, -2 * i / r);             // radians a token
+        if (scaling == FLAT_ROPE_LINEAR) f /= f0;
+        if (scaling == FLAT_ROPE_PARTS) {
+            long double keep = (original_len * f / TWO_PI - low) / (static_cast<long double>(high) - low);
+            keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+            f = (1 - keep) * f / f0 + keep * f;
+        }
+        table[i] = static_cast<uint64_t>(ldexpl(f / TWO_PI, 64) + 0.5L);
+    }
+    *amplitude = scaling == FLAT_ROPE_PARTS ? static_cast<float>(0.1L * logl(f0) + 1) : 1.f;
+    return FLAT_OK;
+}
+
+static int rope(const flat_attn_rope_params_t* p, bool back, void* stream) {
+    const int rc = validate_rope(p);
+    if (rc != FLAT_OK) return rc;
+    const int r = flat::launch_rope(*p, back, static_cast<cudaStream_t>(stream));
+    if (r == FLAT_OK) g_last_launches = 1;
+    return r;
+}
+int flat_attn_rope_fwd(const flat_attn_rope_params_t* p, void* stream) { return rope(p, false, stream); }
+int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream) { return rope(p, true, stream); }
+
+int flat_attn_cache_append(const flat_attn_cache_t* c, const void* K, const void* V, long long total, long long k_stride_t,
+                           long long k_stride_h, long long v_stride_t, long long v_stride_h, int max_new, void* stream) {
+    if (!K || !V) return FLAT_ERR_NULL;
+    const int rc = validate_cache(c);
+    if (rc != FLAT_OK) return rc;
+    const long long strides[4] = {k_stride_t, k_stride_h, v_stride_t, v_stride_h};
+    if (total < 1 || total > 0x7fffffff || max_new < 1 || max_new > total || !strides_ok(strides, 4, 8)) return FLAT_ERR_SHAPE;
+    if (!aligned16(K) || !aligned16(V)) return FLAT_ERR_ALIGN;
+    flat_attn_cache_t q = *c;
+    q.status = status_or_library_word(c->status);
+    const int r = flat::launch_cache_append(q, K, V, total, k_stride_t, k_stride_h, v_stride_t, v_stride_h, max_new, static_cast<cudaStream_t>(stream));
+    if (r == FLAT_OK) g_last_launches = 1;
+    return r;
+}
+
+size_t flat_attn_cache_workspace_bytes(int Hq, int Hkv, int d) {
+    if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || (d != 64 && d != 128)) return 0;
+    return flat::cache_workspace_bytes(d);
+}
+
+int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_params_t* p, void* stream) {
+    if (!p || !p->Q || !p->O || !p->workspace) return FLAT_ERR_NULL;
+    const int rc = validate_cache(c);
+    if (rc != FLAT_OK) return rc;
+    if (p->Hq < 1 || p->total < 1 || p->max_new < 1 || p->max_new > p->total || !isfinite(p->scale)) return FLAT_ERR_SHAPE;
+    if (p->Hq % c->Hkv != 0 || p->Hq / c->Hkv > 128 || (p->causal != 0 && p->causal != 1)) return FLAT_ERR_UNSUPPORTED;
+    if (p->total > 0x7fffffff / p->Hq) return FLAT_ERR_SHAPE;
+    const long long in[2] = {p->q_stride_t, p->q_stride_h}, out[2] = {p->o_stride_t, p->o_stride_h}, size[2] = {p->total, p->Hq};
+    if (!strides_ok(in, 2, 8) || !strides_ok(out, 2, 8) || !apart(out, size, 2, c->d)) return FLAT_ERR_SHAPE;
+    if (!aligned16(p->Q) || !aligned16(p->O) || !aligned(p->workspace, 256) || !aligned(p->lse, 4)) return FLAT_ERR_ALIGN;
+    if (p->workspace_bytes < flat::cache_workspace_bytes(c->d)) return FLAT_ERR_WORKSPACE;
+    flat_attn_cache_t q = *c;
+    q.status = status_or_library_word(c->status);
+    const int r = flat::launch_cache_decode(q, *p, 0x7fffffff, static_cast<cudaStream_t>(stream));
+    if (r == FLAT_OK) g_last_launches = 1;
+    return r;
 }
 
 int flat_attn_last_launch_count(void) { return g_last_launches; }

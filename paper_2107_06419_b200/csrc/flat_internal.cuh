@@ -112,6 +112,14 @@ int launch_fc(const void* X, const void* W, void* Y, int M, int Kdim, int Nout, 
 // The block's normalisation layer (layernorm.cu): Y = gamma * normalise(X + R) + beta over rows of D features.
 int launch_layernorm(const void* X, const void* R, const void* gamma, const void* beta, void* Y, long long M, int D,
                      float eps, cudaStream_t st);
+// Rotary positions (rope.cu); `back`: the gradient.
+int launch_rope(const flat_attn_rope_params_t& p, bool back, cudaStream_t st);
+// The 8-bit paged cache: new tokens into it (cache_append.cu), attention over it (cache_decode.cu: sequences of at most `most_rows`
+// rows, new tokens times query heads a key head).
+int launch_cache_append(const flat_attn_cache_t& c, const void* K, const void* V, int64_t total, long long k_st, long long k_sh,
+                        long long v_st, long long v_sh, int max_new, cudaStream_t st);
+int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& p, int most_rows, cudaStream_t st);
+size_t cache_workspace_bytes(int d);
 int launch_wait_timeout_selftest(int32_t* status, cudaStream_t st);
 int launch_exp2_poly_selftest(const float* x, float* y, int n, cudaStream_t st);
 // Tensor-core versions of the baseline's two contractions (bf16, d in {64,128}, Nk % 8 == 0).

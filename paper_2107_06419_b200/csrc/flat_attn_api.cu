@@ -628,9 +628,25 @@ int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_pa
     if (p->workspace_bytes < flat::cache_workspace_bytes(c->d)) return FLAT_ERR_WORKSPACE;
     flat_attn_cache_t q = *c;
     q.status = status_or_library_word(c->status);
-    const int r = flat::launch_cache_decode(q, *p, 0x7fffffff, static_cast<cudaStream_t>(stream));
-    if (r == FLAT_OK) g_last_launches = 1;
-    return r;
+    // Rows of a sequence and key head (new tokens times heads a group): up to FEW the warp-level products, whose tiles have sixteen
+    // rows, beyond the tcgen05 form, whose tiles have 128.  A call whose longest sequence has more may hold short ones too: both
+    // kernels then, each leaving the other's sequences out.
+    constexpr int FEW = 64;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool many = static_cast<int64_t>(p->max_new) * (p->Hq / c->Hkv) > FEW, few = !many || c->num_seqs > 1;
+    int launches = 0;
+    if (many) {
+        const int r = flat::launch_cache_prefill(q, *p, few ? FEW : 0, st);
+        if (r != FLAT_OK) return r;
+        ++launches;
+    }
+    if (few) {
+        const int r = flat::launch_cache_decode(q, *p, FEW, st);
+        if (r != FLAT_OK) return r;
+        ++launches;
+    }
+    g_last_launches = launches;
+    return FLAT_OK;
 }
 
 int flat_attn_last_launch_count(void) { return g_last_launches; }

@@ -115,10 +115,11 @@ int launch_layernorm(const void* X, const void* R, const void* gamma, const void
 // Rotary positions (rope.cu); `back`: the gradient.
 int launch_rope(const flat_attn_rope_params_t& p, bool back, cudaStream_t st);
 // The 8-bit paged cache: new tokens into it (cache_append.cu), attention over it (cache_decode.cu: sequences of at most `most_rows`
-// rows, new tokens times query heads a key head).
+// rows, new tokens times query heads a key head; cache_prefill.cu: the others).
 int launch_cache_append(const flat_attn_cache_t& c, const void* K, const void* V, int64_t total, long long k_st, long long k_sh,
                         long long v_st, long long v_sh, int max_new, cudaStream_t st);
 int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& p, int most_rows, cudaStream_t st);
+int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& p, int least_rows, cudaStream_t st);    // (more than `least_rows`)
 size_t cache_workspace_bytes(int d);
 int launch_wait_timeout_selftest(int32_t* status, cudaStream_t st);
 int launch_exp2_poly_selftest(const float* x, float* y, int n, cudaStream_t st);

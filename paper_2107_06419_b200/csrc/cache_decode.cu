@@ -31,9 +31,12 @@ using namespace cache;
 
 namespace {
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS, STAGES = 3, CTAS = 2;      // (CTAS: per SM)
+constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int HALF_BYTES = 4096, CHUNK_BYTES = 2 * HALF_BYTES;            // a chunk's keys, then its values
-constexpr int SMEM_BYTES = WARPS * STAGES * CHUNK_BYTES;
+// RG: row groups of eight in a tile.  One: three CTAs an SM and two chunks a warp in the ring; two need the registers of two CTAs.
+__host__ __device__ constexpr int CTAS(int RG) { return RG == 1 ? 3 : 2; }
+__host__ __device__ constexpr int STAGES(int RG) { return RG == 1 ? 2 : 3; }
+__host__ __device__ constexpr int SMEM_BYTES(int RG) { return WARPS * STAGES(RG) * CHUNK_BYTES; }
 constexpr float WEIGHT_SHIFT = 15.f;                                      // weights are kept as 2^15 w
 
 struct DecodeArgs {
@@ -52,13 +55,18 @@ struct DecodeArgs {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool take) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void wait_groups() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void lds16(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+// Two 16 x 16 matrices of bytes (lane i: the address of row i % 16 of matrix i / 16), transposed: r[2 y] holds column g, rows 4 t .. + 3
+// of matrix y, r[2 y + 1] column g + 8 (g = lane / 4, t = lane % 4).
+__device__ __forceinline__ void ldsm_bytes(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 // c (16 x 8) += a (16 x 16) b (16 x 8), half precision in
@@ -66,37 +74,47 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uin
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Two e4m3 (the lower or upper half of a word) as two half-precision numbers.
-__device__ __forceinline__ uint32_t halves(uint32_t two) {
-    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
-    return static_cast<uint32_t>(r.x) | static_cast<uint32_t>(r.y) << 16;
+// Four e4m3 as two pairs of half-precision numbers.
+__device__ __forceinline__ void halves(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
 }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ float quad_max(float v) {
-    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
-    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+// The 8 x 8 matrix of half-precision pairs (lane: row lane / 4, columns 2 (lane % 4), + 1), transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
-__device__ __forceinline__ float quad_sum(float v) {
-    v += __shfl_xor_sync(0xffffffffu, v, 1);
-    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+// Over the lanes of the same lane % 4.
+__device__ __forceinline__ float column_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+}
+__device__ __forceinline__ float column_sum(float v) {
+    v += __shfl_xor_sync(0xffffffffu, v, 4);
+    v += __shfl_xor_sync(0xffffffffu, v, 8);
+    return v + __shfl_xor_sync(0xffffffffu, v, 16);
 }
 __device__ __forceinline__ float two_to(int e) {         // 2^e for any e: 0 below, the largest power above
     e = e < -127 ? -127 : e > 127 ? 127 : e;
     return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
 }
 
-// TEAM: warps of a team (4 or 1).  RG: row groups of eight in a tile (1: no sequence has more than eight rows).
-template <int D, int RG, int TEAM>
-__global__ void __launch_bounds__(THREADS, CTAS)
+// TEAM: warps of a team (4 or 1).  RG: row groups of eight in a tile (1: no sequence has more than eight rows).  SMALL: pages of less
+// than a chunk.
+template <int D, int RG, int TEAM, bool SMALL>
+__global__ void __launch_bounds__(THREADS, CTAS(RG))
 cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     constexpr int CH = HALF_BYTES / D;                   // tokens of a chunk: 32 (d = 128) or 64
     constexpr int PIECES = D / 16, RPI = 32 / PIECES;    // 16-byte pieces of a row; rows that a copy instruction brings
-    constexpr int NT = CH / 8;                           // logit blocks of eight keys
+    constexpr int NT = CH / 16;                          // logit blocks of sixteen keys
+    constexpr int STAGES = flat::STAGES(RG);
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int ids[WARPS][STAGES][4];                // the chunk's pages; -1: none there
+    __shared__ int places[WARPS][STAGES][4];             // page and head of the chunk's slots; -1: no page there
     __shared__ long long prefix[THREADS + 1];
     __shared__ float warp_lse[WARPS][16];
     __shared__ int last_word;
@@ -162,9 +180,14 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     }
 
     const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * CHUNK_BYTES;
-    const int page_mask = cv.page - 1, slots = CH >> cv.page_shift > 0 ? CH >> cv.page_shift : 1;
-    // ldmatrix row of the lane: blocks (keys 0-7, piece x), (8-15, x), (0-7, x + 1), (8-15, x + 1)
-    const int vrow = (lane & 7) + ((lane >> 3) & 1) * 8, vpiece = lane >> 4;
+    const int page_mask = cv.page - 1, slots = SMALL ? CH >> cv.page_shift : 1;
+    // ldmatrix row of the lane: sixteen keys of piece x, of piece x + 1
+    const int vrow = lane & 15, vpiece = lane >> 4;
+    // copies: the lane's place in 512 bytes (RPI rows), keys' pieces of odd rows changed by four, values' by the row
+    const int crow = lane / PIECES, piece = lane % PIECES;
+    // logits: rows g and g + 8 of a block of sixteen keys are the keys krow and krow + 2, so that the weights that a lane holds as
+    // the right operand (rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9) are those of the keys 4 t .. 4 t + 3
+    const int krow = 4 * (g >> 1) + (g & 1);
 
     while (pos < end) {
         while (pos >= base + chunks) { base += chunks; ++s; chunks = shape(s, sp, nch, tiles); }
@@ -178,213 +201,281 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         // ------------------------------------------------------------ copies
         const int count = a1 - a0 - member <= 0 ? 0 : (a1 - a0 - member + TEAM - 1) / TEAM;     // this warp's chunks
         const int pages = (sp.len + page_mask) >> cv.page_shift;
-        auto load_id = [&](int k) {                      // lane j: the page of the k-th chunk's j-th slot
-            const int chunk = a0 + member + k * TEAM, index = (chunk * CH >> cv.page_shift) + lane;
-            int id = -1;
-            if (k < count && lane < slots && index < pages && !read_page(cv, s, index, id)) id = -1;
-            return id;
+        const int32_t* table = cv.table + static_cast<int64_t>(s) * cv.max_pages;
+        // Of the k-th chunk: page * heads + head; -1: no page.  SMALL: lane j that of the j-th slot; otherwise every lane the same.
+        auto load_place = [&](int k) {
+            const int index = ((a0 + member + k * TEAM) * CH >> cv.page_shift) + (SMALL ? lane : 0);
+            if (k >= count || index >= pages || (SMALL && lane >= slots)) return -1;
+            const int id = table[index];
+            if (id < 0 || id >= cv.num_pages) {
+                if (cv.status) atomicExch(cv.status, FLAT_CACHE_BAD_PAGE);
+                return -1;
+            }
+            return id * cv.Hkv + h;
         };
-        auto issue = [&](int k, int id) {
+        auto issue = [&](int k, int place) {
             if (k < count) {
                 const int st = k % STAGES, key0 = (a0 + member + k * TEAM) * CH;
-                if (lane < 4) ids[warp][st][lane] = id;
-                const long long off = ((static_cast<long long>(id < 0 ? 0 : id) * cv.Hkv + h) << cv.page_shift) * D;
-                const uint32_t dst = ring + st * CHUNK_BYTES;
+                if (lane < (SMALL ? 4 : 1)) places[warp][st][lane] = place;
+                const int64_t off = (static_cast<int64_t>(place < 0 ? 0 : place) << cv.page_shift) * D + lane * 16;
+                const uint32_t dst = ring + st * CHUNK_BYTES + crow * D;
+                const bool full = key0 + CH <= sp.len && (SMALL ? __all_sync(0xffffffffu, place >= 0 || lane >= slots) : place >= 0);
+                // sixteen tokens of a page and head are contiguous: a pointer for them, 512 bytes a copy instruction
 #pragma unroll
-                for (int i = 0; i < CH / RPI; ++i) {
-                    const int slot = (i * RPI) >> cv.page_shift, row = i * RPI + lane / PIECES, piece = lane % PIECES;
-                    const long long o = __shfl_sync(0xffffffffu, off, slot);
-                    const bool take = __shfl_sync(0xffffffffu, id, slot) >= 0 && key0 + row < sp.len;
-                    const long long src = o + ((key0 + row) & page_mask) * D + piece * 16;
-                    // (keys: pieces of odd rows change places by four; values: by the row, so that ldmatrix meets eight different banks)
-                    const int kp = D == 128 ? piece ^ ((row & 1) << 2) : piece, vp = D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3);
-                    copy16(dst + row * D + kp * 16, cv.k + src, take);
-                    copy16(dst + HALF_BYTES + row * D + vp * 16, cv.v + src, take);
+                for (int u = 0; u < CH / 16; ++u) {
+                    int64_t o = off;
+                    bool there = place >= 0;
+                    if (SMALL) {
+                        const int slot = (u * 16) >> cv.page_shift;
+                        o = __shfl_sync(0xffffffffu, off - lane * 16, slot) + lane * 16;
+                        there = __shfl_sync(0xffffffffu, place, slot) >= 0;
+                    }
+                    o += ((key0 + 16 * u) & page_mask) * D;
+                    const uint8_t *ks = cv.k + o, *vs = cv.v + o;
+#pragma unroll
+                    for (int i = 0; i < 16 / RPI; ++i) {
+                        const int row = u * 16 + i * RPI;        // (of lane 0's piece)
+                        const int kp = D == 128 ? piece ^ ((crow & 1) << 2) : piece, vp = D == 128 ? piece ^ ((row + crow) & 7) : piece ^ ((crow >> 1) & 3);
+                        const uint32_t kd = dst + row * D + kp * 16, vd = dst + HALF_BYTES + row * D + vp * 16;
+                        if (full) {
+                            copy16(kd, ks + i * 512);
+                            copy16(vd, vs + i * 512);
+                        } else {
+                            const bool take = there && key0 + row + crow < sp.len;
+                            copy16(kd, ks + i * 512, take);
+                            copy16(vd, vs + i * 512, take);
+                        }
+                    }
                 }
             }
             commit();
         };
-        auto load_exps = [&](int k, int& ek, int& ev) {  // lane j: of the k-th chunk's j-th slot
+        auto load_exps = [&](int k, int& ek, int& ev) {  // of the places of the k-th chunk
             ek = ev = 0;
-            if (k < count && lane < slots) {
-                const int id = ids[warp][k % STAGES][lane];
-                if (id >= 0) {
-                    const long long at = static_cast<long long>(id) * cv.Hkv + h;
-                    ek = cv.k_exp[at];
-                    ev = cv.v_exp[at];
+            if (k < count && (!SMALL || lane < slots)) {
+                const int place = places[warp][k % STAGES][SMALL ? lane : 0];
+                if (place >= 0) {
+                    ek = cv.k_exp[place];
+                    ev = cv.v_exp[place];
                 }
             }
         };
         {
-            int id = load_id(0);
+            int id = load_place(0);
 #pragma unroll
             for (int k = 0; k < STAGES - 1; ++k) {
-                const int next = load_id(k + 1);
+                const int next = load_place(k + 1);
                 issue(k, id);
                 id = next;
             }
         }
-        int id_next = load_id(STAGES - 1);
+        int place_next = load_place(STAGES - 1);
         __syncwarp();
         int ek_next, ev_next;
         load_exps(0, ek_next, ev_next);
 
         // ------------------------------------------------------------ queries: half precision, a power of two taken out of each row
-        // Slice (x, w) of the contraction: a lane's features 16 (t + 4 x) + 4 w .. + 3, the ones that it reads of a key
-        uint32_t qa[D / 16][4];
-        float unit[RG];
-        int nrow[RG];
-        {
-            uint4 raw[RG][D / 64][2];
+        // Slice 4 x + w of the contraction: a lane's features 16 (t + 4 x) + 4 w .. + 3, the ones that it reads of a key
+        uint32_t qb[D / 16][RG][2];
+        float unit[RG][2];                               // of the rows 8 r + 2 t, + 1: logits' scale, keys that they see
+        int nrow[RG][2];
 #pragma unroll
-            for (int r = 0; r < RG; ++r) {
-                const int row = g + 8 * r;
-                float top = 0.f;
-                const int flat_row = tile * 16 + row, tok = flat_row / p.G, gh = flat_row - tok * p.G;
+        for (int r = 0; r < RG; ++r) {
+            const int row = g + 8 * r, flat_row = tile * 16 + row, tok = flat_row / p.G, gh = flat_row - tok * p.G;
+            uint4 raw[D / 64][2];
+            float top = 0.f;
 #pragma unroll
-                for (int x = 0; x < D / 64; ++x)
+            for (int x = 0; x < D / 64; ++x)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        raw[r][x][e] = make_uint4(0, 0, 0, 0);
-                        if (row < rows)
-                            raw[r][x][e] = reinterpret_cast<const uint4*>(p.Q + (sp.q0 + tok) * p.q_st + (static_cast<long long>(h) * p.G + gh) * p.q_sh + 16 * (t + 4 * x))[e];
-                        const uint32_t w[4] = {raw[r][x][e].x, raw[r][x][e].y, raw[r][x][e].z, raw[r][x][e].w};
+                for (int e = 0; e < 2; ++e) {
+                    raw[x][e] = make_uint4(0, 0, 0, 0);
+                    if (row < rows)
+                        raw[x][e] = reinterpret_cast<const uint4*>(p.Q + (sp.q0 + tok) * p.q_st + (static_cast<long long>(h) * p.G + gh) * p.q_sh + 16 * (t + 4 * x))[e];
+                    const uint32_t w[4] = {raw[x][e].x, raw[x][e].y, raw[x][e].z, raw[x][e].w};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
-                    }
-                top = quad_max(top);
-                int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;      // the row's largest: 2^e to 2^(e + 1)
-                e = e < -100 ? -100 : e;
-                const float up = two_to(14 - e);
-                unit[r] = p.scale_log2e * two_to(e - 14);
-                const long long lim = static_cast<long long>(tok) + 1 + sp.len - sp.n;
-                nrow[r] = row < rows ? (p.causal && lim < sp.len ? static_cast<int>(lim) : sp.len) : 0;
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+                }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;          // the row's largest: 2^e to 2^(e + 1)
+            e = e < -100 ? -100 : e;
+            const float up = two_to(14 - e), down = p.scale_log2e * two_to(e - 14);
+            const long long lim = static_cast<long long>(tok) + 1 + sp.len - sp.n;
+            const int seen = row < rows ? (p.causal && lim < sp.len ? static_cast<int>(lim) : sp.len) : 0;
 #pragma unroll
-                for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint4& v = raw[r][x][w >> 1];
-                        const uint32_t lo = w & 1 ? v.z : v.x, hi = w & 1 ? v.w : v.y;
-                        qa[4 * x + w][r] = pack_half2(__uint_as_float(lo << 16) * up, __uint_as_float(lo & 0xffff0000u) * up);
-                        qa[4 * x + w][2 + r] = pack_half2(__uint_as_float(hi << 16) * up, __uint_as_float(hi & 0xffff0000u) * up);
-                        if (RG == 1) qa[4 * x + w][1] = qa[4 * x + w][3] = 0u;
-                    }
+            for (int y = 0; y < 2; ++y) {
+                unit[r][y] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + y));
+                nrow[r][y] = __shfl_sync(0xffffffffu, seen, 4 * (2 * t + y));
             }
+#pragma unroll
+            for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint4& v = raw[x][w >> 1];
+                    const uint32_t lo = w & 1 ? v.z : v.x, hi = w & 1 ? v.w : v.y;
+                    qb[4 * x + w][r][0] = pack_half2(__uint_as_float(lo << 16) * up, __uint_as_float(lo & 0xffff0000u) * up);
+                    qb[4 * x + w][r][1] = pack_half2(__uint_as_float(hi << 16) * up, __uint_as_float(hi & 0xffff0000u) * up);
+                }
         }
         const long long lim0 = static_cast<long long>(tile * 16 / p.G) + 1 + sp.len - sp.n;     // keys that every row sees
         const int nmin = p.causal && lim0 < sp.len ? static_cast<int>(lim0) : sp.len;
 
         // ------------------------------------------------------------ the chunks
-        float o[D / 8][4], m[RG], l[RG];
+        // o[x][r]: features 16 x + g (0, 1) and 16 x + g + 8 (2, 3) of the rows 8 r + 2 t and 8 r + 2 t + 1
+        float o[PIECES][RG][4], m[RG][2], l[RG][2];
         int E = -1000;                                   // o is in units of 2^E
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i)
+        for (int r = 0; r < RG; ++r) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+            for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-        for (int r = 0; r < RG; ++r) { m[r] = -INFINITY; l[r] = 0.f; }
+                for (int e = 0; e < 4; ++e) o[i][r][e] = 0.f;
+            m[r][0] = m[r][1] = -INFINITY;
+            l[r][0] = l[r][1] = 0.f;
+        }
         for (int k = 0; k < count; ++k) {
             const int st = k % STAGES, key0 = (a0 + member + k * TEAM) * CH;
             wait_groups<STAGES - 2>();
             __syncwarp();
             const int ek = ek_next, ev = ev_next;
             // bit j: slot j has no page
-            const int bad = __ballot_sync(0xffffffffu, lane < slots && ids[warp][st][lane & 3] < 0);
-            issue(k + STAGES - 1, id_next);              // (into the stage that every lane had read before this chunk's barrier)
-            id_next = load_id(k + STAGES);
+            const int bad = SMALL ? __ballot_sync(0xffffffffu, lane < slots && places[warp][st][lane & 3] < 0) : places[warp][st][0] < 0;
+            issue(k + STAGES - 1, place_next);           // (into the stage that every lane had read before this chunk's barrier)
+            place_next = load_place(k + STAGES);
             const uint32_t ks = ring + st * CHUNK_BYTES, vs = ks + HALF_BYTES;
-            float c[NT][4];
+            // logits, keys as rows: c[i][r]: keys 16 i + krow (0, 1) and 16 i + krow + 2 (2, 3) of the rows 8 r + 2 t and 8 r + 2 t + 1
+            float c[NT][RG][4];
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) c[i][e] = 0.f;
-                const int row = i * 8 + g;
+                for (int r = 0; r < RG; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) c[i][r][e] = 0.f;
+                const uint32_t row = ks + (i * 16 + krow) * D;
 #pragma unroll
                 for (int x = 0; x < D / 64; ++x) {
-                    uint32_t w[4];
-                    lds16(ks + row * D + (D == 128 ? (t + 4 * x) ^ ((row & 1) << 2) : t) * 16, w);
+                    uint32_t w[4], v[4];
+                    const int at = (D == 128 ? (t + 4 * x) ^ ((krow & 1) << 2) : t) * 16;
+                    lds16(row + at, w);
+                    lds16(row + 2 * D + at, v);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) mma16(c[i], qa[4 * x + e], halves(w[e] & 0xffffu), halves(w[e] >> 16));
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t a[4];
+                        halves(w[e], a[0], a[2]);
+                        halves(v[e], a[1], a[3]);
+#pragma unroll
+                        for (int r = 0; r < RG; ++r) mma16(c[i][r], a, qb[4 * x + e][r][0], qb[4 * x + e][r][1]);
+                    }
                 }
             }
             // base-2 logits; keys that a row does not see take no part
             const bool masked = key0 + CH > nmin || bad != 0;
-            float mx[RG], wv[NT / 2];                    // wv: what the weights of sixteen keys are multiplied by for their values' scale
-            int e_top = -1000;
+            float uk[NT], wv[NT];                        // of sixteen keys: their scale; what their weights are multiplied by for their values' scale
+            int evs[NT], e_top = -1000;
+            const float ek_scale = two_to(ek - 127);
 #pragma unroll
-            for (int i = 0; i < NT / 2; ++i) {
-                const int v = __shfl_sync(0xffffffffu, ev, (i * 16) >> cv.page_shift);
-                wv[i] = __int_as_float(v);
-                if (v > e_top) e_top = v;
+            for (int i = 0; i < NT; ++i) {
+                uk[i] = SMALL ? __shfl_sync(0xffffffffu, ek_scale, (i * 16) >> cv.page_shift) : ek_scale;
+                evs[i] = SMALL ? __shfl_sync(0xffffffffu, ev, (i * 16) >> cv.page_shift) : ev;
+                e_top = max(e_top, evs[i]);
             }
-            bool grown = false;
             if (e_top > E) {
                 const float down = E < -500 ? 0.f : two_to(E - e_top);
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i)
+                for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[i][e] *= down;
+                    for (int r = 0; r < RG; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[i][r][e] *= down;
                 E = e_top;
             }
 #pragma unroll
-            for (int i = 0; i < NT / 2; ++i) wv[i] = two_to(__float_as_int(wv[i]) - E);
+            for (int i = 0; i < NT; ++i) wv[i] = two_to(evs[i] - E);
+            bool grown = false;
+            float mx[RG][2];
 #pragma unroll
-            for (int r = 0; r < RG; ++r) {
-                mx[r] = -INFINITY;
+            for (int r = 0; r < RG; ++r)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        const float u = unit[r][y] * uk[i];
+                        c[i][r][y] *= u;
+                        c[i][r][2 + y] *= u;
+                    }
+            if (masked) {
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
-                    const int slot = (i * 8) >> cv.page_shift;
-                    const float u = unit[r] * two_to(__shfl_sync(0xffffffffu, ek, slot) - 127);
+                    const int key = key0 + i * 16 + krow;
+                    const bool gone = bad >> (SMALL ? (i * 16) >> cv.page_shift : 0) & 1;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float x = c[i][2 * r + e] * u;
-                        if (masked && (key0 + i * 8 + 2 * t + e >= nrow[r] || (bad >> slot & 1))) x = -INFINITY;
-                        c[i][2 * r + e] = x;
-                        mx[r] = fmaxf(mx[r], x);
-                    }
+                    for (int r = 0; r < RG; ++r)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            if (gone || key >= nrow[r][y]) c[i][r][y] = -INFINITY;
+                            if (gone || key + 2 >= nrow[r][y]) c[i][r][2 + y] = -INFINITY;
+                        }
                 }
-                mx[r] = quad_max(mx[r]);
-                grown = grown || mx[r] > m[r];
             }
+#pragma unroll
+            for (int r = 0; r < RG; ++r)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    mx[r][y] = fmaxf(c[0][r][y], c[0][r][2 + y]);
+#pragma unroll
+                    for (int i = 1; i < NT; ++i) mx[r][y] = tc::max3(mx[r][y], c[i][r][y], c[i][r][2 + y]);
+                    grown = grown || mx[r][y] > m[r][y];
+                }
+            // (the maximum is taken over the lanes only where one of them has met a larger logit)
             if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-                for (int r = 0; r < RG; ++r) {
-                    const float mn = fmaxf(m[r], mx[r]);
-                    const float a = mn == -INFINITY ? 1.f : tc::ex2_approx(m[r] - mn);
-                    m[r] = mn;
-                    l[r] *= a;
+                for (int r = 0; r < RG; ++r)
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) { o[i][2 * r] *= a; o[i][2 * r + 1] *= a; }
+                    for (int y = 0; y < 2; ++y) {
+                        const float mn = fmaxf(m[r][y], column_max(mx[r][y]));
+                        const float a = mn == -INFINITY ? 1.f : tc::ex2_approx(m[r][y] - mn);
+                        m[r][y] = mn;
+                        l[r][y] *= a;
+#pragma unroll
+                        for (int i = 0; i < PIECES; ++i) { o[i][r][y] *= a; o[i][r][2 + y] *= a; }
+                    }
+            }
+            uint32_t pb[NT][RG][2];                      // weights as the right operand
+#pragma unroll
+            for (int r = 0; r < RG; ++r) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float ref = m[r][y] == -INFINITY ? 0.f : m[r][y] - WEIGHT_SHIFT;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float w = tc::ex2_approx(c[i][r][2 * e + y] - ref);
+                            l[r][y] += w;
+                            c[i][r][2 * e + y] = w * wv[i];
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    pb[i][r][0] = transpose8(pack_half2(c[i][r][0], c[i][r][1]));
+                    pb[i][r][1] = transpose8(pack_half2(c[i][r][2], c[i][r][3]));
                 }
             }
 #pragma unroll
-            for (int r = 0; r < RG; ++r) {
-                const float ref = m[r] == -INFINITY ? 0.f : m[r] - WEIGHT_SHIFT;
-#pragma unroll
-                for (int i = 0; i < NT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float w = tc::ex2_approx(c[i][2 * r + e] - ref);
-                        l[r] += w;
-                        c[i][2 * r + e] = w * wv[i / 2];
-                    }
-            }
-#pragma unroll
-            for (int i = 0; i < NT; i += 2) {
-                const uint32_t pa[4] = {pack_half2(c[i][0], c[i][1]), RG == 2 ? pack_half2(c[i][2], c[i][3]) : 0u,
-                                        pack_half2(c[i + 1][0], c[i + 1][1]), RG == 2 ? pack_half2(c[i + 1][2], c[i + 1][3]) : 0u};
-                const int row = i * 8 + vrow;
+            for (int i = 0; i < NT; ++i) {
+                const int row = i * 16 + vrow;
 #pragma unroll
                 for (int x = 0; x < PIECES; x += 2) {
                     const int piece = x + vpiece;
                     uint32_t b[4];
-                    ldsm4_t(vs + row * D + (D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3)) * 16, b);
-                    // a word: features 2 g, 2 g + 1 of key 2 t, then of key 2 t + 1
+                    ldsm_bytes(vs + row * D + (D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3)) * 16, b);
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const uint32_t lo = __byte_perm(b[2 * y], 0, 0x3120), hi = __byte_perm(b[2 * y + 1], 0, 0x3120);
-                        mma16(o[2 * (x + y)], pa, halves(lo & 0xffffu), halves(hi & 0xffffu));
-                        mma16(o[2 * (x + y) + 1], pa, halves(lo >> 16), halves(hi >> 16));
+                        uint32_t a[4];                   // rows g, g + 8: features 16 (x + y) + g, + 8
+                        halves(b[2 * y], a[0], a[2]);
+                        halves(b[2 * y + 1], a[1], a[3]);
+#pragma unroll
+                        for (int r = 0; r < RG; ++r) mma16(o[x + y][r], a, pb[i][r][0], pb[i][r][1]);
                     }
                 }
             }
@@ -393,16 +484,16 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         wait_groups<0>();
 
         // ------------------------------------------------------------ normalised outputs and log-sums of this warp's keys
-        // o[2 x], o[2 x + 1] of row r: features 16 x + 4 t + {0, 2}, {1, 3}
-        float lg[RG];
+        float lg[RG][2];
 #pragma unroll
-        for (int r = 0; r < RG; ++r) {
-            l[r] = quad_sum(l[r]);
-            const float inv = l[r] > 0.f ? two_to(E - 127) / l[r] : l[r] == l[r] ? 0.f : l[r];
-            lg[r] = l[r] > 0.f ? m[r] - WEIGHT_SHIFT + log2f(l[r]) : l[r] == l[r] ? -INFINITY : l[r];
+        for (int r = 0; r < RG; ++r)
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) { o[i][2 * r] *= inv; o[i][2 * r + 1] *= inv; }
-        }
+            for (int y = 0; y < 2; ++y) {
+                const float sum = column_sum(l[r][y]), inv = sum > 0.f ? two_to(E - 127) / sum : sum == sum ? 0.f : sum;
+                lg[r][y] = sum > 0.f ? m[r][y] - WEIGHT_SHIFT + log2f(sum) : sum == sum ? -INFINITY : sum;
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) { o[i][r][y] *= inv; o[i][r][2 + y] *= inv; }
+            }
         const bool whole = a0 == 0 && a1 == nch;
         const long long first_team = item_begin / share, last_team = (item_begin + nch - 1) / share;
         const long long slot = 2 * team + (pos == begin ? 0 : 1);
@@ -416,30 +507,40 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         };
         if (TEAM == 1) {
 #pragma unroll
-            for (int r = 0; r < RG; ++r) {
-                const int row = g + 8 * r;
-                if (row >= rows) continue;
+            for (int r = 0; r < RG; ++r)
 #pragma unroll
-                for (int x = 0; x < PIECES; ++x) {
-                    const float4 v = make_float4(o[2 * x][2 * r], o[2 * x + 1][2 * r], o[2 * x][2 * r + 1], o[2 * x + 1][2 * r + 1]);
-                    if (whole) finish(row, 16 * x + 4 * t, v, lg[r]);
-                    else *reinterpret_cast<float4*>(p.part_o + (slot * 16 + row) * D + 16 * x + 4 * t) = v;
+                for (int y = 0; y < 2; ++y) {
+                    const int row = 8 * r + 2 * t + y;
+                    if (row >= rows) continue;
+                    const int flat_row = tile * 16 + row, tok = flat_row / p.G, head = h * p.G + flat_row - tok * p.G;
+                    __nv_bfloat16* out = p.O + (sp.q0 + tok) * p.o_st + head * p.o_sh + g;
+                    float* part = p.part_o + (slot * 16 + row) * D + g;
+#pragma unroll
+                    for (int x = 0; x < PIECES; ++x)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (whole) out[16 * x + 8 * e] = __float2bfloat16(o[x][r][2 * e + y]);
+                            else part[16 * x + 8 * e] = o[x][r][2 * e + y];
+                        }
+                    if (g == 0 && !whole) p.part_lse[slot * 16 + row] = lg[r][y];
+                    if (g == 0 && whole && p.lse) p.lse[static_cast<long long>(sp.q0 + tok) * p.Hq + head] = lg[r][y] * 0.6931471805599453f;
                 }
-                if (!whole && t == 0) p.part_lse[slot * 16 + row] = lg[r];
-            }
         } else {
             // the team's warps join through the memory of their rings
             __syncthreads();
             float* parts = reinterpret_cast<float*>(smem);                // [warp][row][D]
 #pragma unroll
-            for (int r = 0; r < RG; ++r) {
-                const int row = g + 8 * r;
+            for (int r = 0; r < RG; ++r)
 #pragma unroll
-                for (int x = 0; x < PIECES; ++x)
-                    *reinterpret_cast<float4*>(parts + (warp * 16 + row) * D + 16 * x + 4 * t) =
-                        make_float4(o[2 * x][2 * r], o[2 * x + 1][2 * r], o[2 * x][2 * r + 1], o[2 * x + 1][2 * r + 1]);
-                if (t == 0) warp_lse[warp][row] = lg[r];
-            }
+                for (int y = 0; y < 2; ++y) {
+                    const int row = 8 * r + 2 * t + y;
+#pragma unroll
+                    for (int x = 0; x < PIECES; ++x) {
+                        parts[(warp * 16 + row) * D + 16 * x + g] = o[x][r][y];
+                        parts[(warp * 16 + row) * D + 16 * x + 8 + g] = o[x][r][2 + y];
+                    }
+                    if (g == 0) warp_lse[warp][row] = lg[r][y];
+                }
             __syncthreads();
             for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
                 const int row = i / (D / 4), col = i % (D / 4) * 4;
@@ -530,15 +631,38 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 
 }  // namespace
 
+namespace {
+size_t most_teams() { return static_cast<size_t>(device_sm_count()) * 3 * WARPS; }     // (three CTAs an SM, a team a warp)
+size_t counter_bytes() { return (most_teams() * sizeof(int) + 255) & ~size_t(255); }
+
+template <int D, int RG, int TEAM, bool SMALL>
+int launch(const DecodeArgs& p, cudaStream_t st) {
+    if (!ensure_dynamic_smem<cache_decode_kernel<D, RG, TEAM, SMALL>>(SMEM_BYTES(RG))) return FLAT_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(device_sm_count() * CTAS(RG));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM_BYTES(RG);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, cache_decode_kernel<D, RG, TEAM, SMALL>, p) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA;
+}
+template <int D, int RG>
+int launch_form(const DecodeArgs& p, bool by_warp, cudaStream_t st) {
+    const bool small = p.c.page < HALF_BYTES / D;
+    if (by_warp) return small ? launch<D, RG, 1, true>(p, st) : launch<D, RG, 1, false>(p, st);
+    return small ? launch<D, RG, WARPS, true>(p, st) : launch<D, RG, WARPS, false>(p, st);
+}
+}  // namespace
+
 size_t cache_workspace_bytes(int d) {
-    const size_t teams = static_cast<size_t>(device_sm_count()) * CTAS * WARPS;
-    const size_t counters = (teams * sizeof(int) + 255) & ~size_t(255);
-    return counters + 2 * teams * 16 * sizeof(float) + 2 * teams * 16 * d * sizeof(float);
+    return counter_bytes() + 2 * most_teams() * 16 * sizeof(float) + 2 * most_teams() * 16 * d * sizeof(float);
 }
 
 int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int most_rows, cudaStream_t st) {
-    const int sms = device_sm_count();
-    const size_t teams = static_cast<size_t>(sms) * CTAS * WARPS;
     DecodeArgs p{};
     p.c = cache_view(c);
     p.Q = static_cast<const __nv_bfloat16*>(q.Q);
@@ -550,33 +674,13 @@ int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_pa
     p.scale_log2e = q.scale * 1.4426950408889634f;
     char* w = static_cast<char*>(q.workspace);
     p.counters = reinterpret_cast<int*>(w);
-    p.part_lse = reinterpret_cast<float*>(w + ((teams * sizeof(int) + 255) & ~size_t(255)));
-    p.part_o = p.part_lse + 2 * teams * 16;
-    const int64_t rows = static_cast<int64_t>(q.max_new) * p.G, least = rows < most_rows ? rows : most_rows;
-    const int64_t items = static_cast<int64_t>(c.num_seqs) * c.Hkv * ((least + 15) / 16);
-    const bool by_warp = items >= static_cast<int64_t>(teams);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(sms * CTAS);
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = SMEM_BYTES;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    auto go = [&](auto kernel_ok, void (*kern)(DecodeArgs)) {
-        if (!kernel_ok) return static_cast<int>(FLAT_ERR_CUDA);
-        return static_cast<int>(cudaLaunchKernelEx(&cfg, kern, p) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA);
-    };
-#define FLAT_DECODE(DD, RG, TEAM) go(ensure_dynamic_smem<cache_decode_kernel<DD, RG, TEAM>>(SMEM_BYTES), cache_decode_kernel<DD, RG, TEAM>)
-    if (c.d == 64) {
-        if (rows <= 8) return by_warp ? FLAT_DECODE(64, 1, 1) : FLAT_DECODE(64, 1, 4);
-        return by_warp ? FLAT_DECODE(64, 2, 1) : FLAT_DECODE(64, 2, 4);
-    }
-    if (rows <= 8) return by_warp ? FLAT_DECODE(128, 1, 1) : FLAT_DECODE(128, 1, 4);
-    return by_warp ? FLAT_DECODE(128, 2, 1) : FLAT_DECODE(128, 2, 4);
-#undef FLAT_DECODE
+    p.part_lse = reinterpret_cast<float*>(w + counter_bytes());
+    p.part_o = p.part_lse + 2 * most_teams() * 16;
+    const int64_t rows = static_cast<int64_t>(q.max_new) * p.G, most = rows < most_rows ? rows : most_rows;
+    const int64_t items = static_cast<int64_t>(c.num_seqs) * c.Hkv * ((most + 15) / 16);
+    const bool by_warp = items >= static_cast<int64_t>(most_teams());
+    if (c.d == 64) return rows <= 8 ? launch_form<64, 1>(p, by_warp, st) : launch_form<64, 2>(p, by_warp, st);
+    return rows <= 8 ? launch_form<128, 1>(p, by_warp, st) : launch_form<128, 2>(p, by_warp, st);
 }
 
 }  // namespace flat

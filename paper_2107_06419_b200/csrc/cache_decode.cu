@@ -37,6 +37,10 @@ constexpr int HALF_BYTES = 4096, CHUNK_BYTES = 2 * HALF_BYTES;            // a c
 __host__ __device__ constexpr int CTAS(int RG) { return RG == 1 ? 3 : 2; }
 __host__ __device__ constexpr int STAGES(int RG) { return RG == 1 ? 2 : 3; }
 __host__ __device__ constexpr int SMEM_BYTES(int RG) { return WARPS * STAGES(RG) * CHUNK_BYTES; }
+constexpr int ALIGN_COST = 5;                                             // chunks
+// Aligned parts have at least this many chunks, one a warp; of a long item more: its parts are joined one after the other, sixteen in
+// flight (0.03 us each), a warp's chunk takes 0.6 us, so P parts of n chunks take about n / (4 P) 0.6 + 0.03 P us, least at P = sqrt(5 n).
+__device__ __forceinline__ int least_part(int n) { return max(WARPS, static_cast<int>(sqrtf(0.2f * n)) + 1); }
 constexpr float WEIGHT_SHIFT = 15.f;                                      // weights are kept as 2^15 w
 
 struct DecodeArgs {
@@ -114,7 +118,6 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     constexpr int NT = CH / 16;                          // logit blocks of sixteen keys
     constexpr int STAGES = flat::STAGES(RG);
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int places[WARPS][STAGES][4];             // page and head of the chunk's slots; -1: no page there
     __shared__ long long prefix[THREADS + 1];
     __shared__ float warp_lse[WARPS][16];
     __shared__ int last_word;
@@ -135,20 +138,59 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         nch = (sp.len + CH - 1) / CH;
         return static_cast<long long>(nch) * tiles * cv.Hkv;
     };
-    const int per = (cv.num_seqs + THREADS - 1) / THREADS;
-    {
+    const int per = (cv.num_seqs + THREADS - 1) / THREADS, s_begin = threadIdx.x * per;
+    const int s_end = s_begin + per < cv.num_seqs ? s_begin + per : cv.num_seqs;
+    int nch, tiles;
+    Span sp;
+    long long units = 0, items = 0;
+    for (int s = s_begin; s < s_end; ++s) {
+        units += shape(s, sp, nch, tiles);
+        items += static_cast<long long>(tiles) * cv.Hkv;
+    }
+    auto block_sum = [&](long long v) {                  // (called by every thread)
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        __syncthreads();
+        if (lane == 0) prefix[warp] = v;
+        __syncthreads();
         long long sum = 0;
-        for (int i = 0; i < per; ++i) {
-            const int s = threadIdx.x * per + i;
-            Span sp;
-            int a, b;
-            if (s < cv.num_seqs) sum += shape(s, sp, a, b);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) sum += prefix[w];
+        return sum;
+    };
+    const long long chunks_all = block_sum(units);
+    // An equal share of the chunks each.  Where there are less than half as many items as teams, and it costs no team more than ALIGN_COST
+    // chunks, every team has a part of one item instead, and an item's parts are alike: a team that goes from one item to the next
+    // pays for two (about as long as ALIGN_COST chunks).
+    long long share = (chunks_all + teams - 1) / teams;
+    int aligned = 0;                                     // chunks of a part, at least
+    auto pieces = [&](int n) {                           // parts of an item of n chunks
+        const int c = max(aligned, least_part(n));
+        return (n + c - 1) / c;
+    };
+    if (TEAM > 1) {
+        const long long items_all = block_sum(items);
+        if (2 * items_all <= teams) {
+            const long long c = (chunks_all + teams - items_all - 1) / (teams - items_all);
+            if (c <= share + ALIGN_COST) aligned = static_cast<int>(c);
         }
+        if (aligned) {
+            share = 1;
+            units = 0;
+            for (int s = s_begin; s < s_end; ++s) {
+                shape(s, sp, nch, tiles);
+                units += static_cast<long long>(tiles) * cv.Hkv * pieces(nch);
+            }
+        }
+    }
+    {   // the sequences' first units
+        long long sum = units;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long v = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += v;
         }
+        __syncthreads();
         prefix[threadIdx.x + 1] = sum;
         if (threadIdx.x == 0) prefix[0] = 0;
         __syncthreads();
@@ -159,15 +201,17 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         __syncthreads();
     }
     const long long all = prefix[THREADS];
-    // an equal share each, of at least two chunks a warp
-    long long share = (all + teams - 1) / teams;
-    if (share < 2 * TEAM) share = 2 * TEAM;
     long long pos = team * share;
     const long long begin = pos, end = pos + share < all ? pos + share : all;
     if (TEAM > 1 && pos >= end) return;                  // (the whole CTA)
-    int s = 0, nch = 0, tiles = 0;
-    Span sp{};
-    long long base = 0, chunks = 0;
+    int s = 0;
+    long long base = 0;
+    nch = tiles = 0;
+    units = 0;                                           // now: of sequence s, which begins with unit `base`
+    auto look = [&](int s) {
+        const long long chunks = shape(s, sp, nch, tiles);
+        return TEAM > 1 && aligned ? static_cast<long long>(tiles) * cv.Hkv * pieces(nch) : chunks;
+    };
     if (pos < end) {
         int lo = 0, hi = THREADS;                        // the last thread whose sequences begin at or before pos
         while (hi - lo > 1) {
@@ -176,7 +220,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         }
         s = lo * per;
         base = prefix[lo];
-        chunks = shape(s, sp, nch, tiles);
+        units = look(s);
     }
 
     const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * CHUNK_BYTES;
@@ -190,13 +234,23 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     const int krow = 4 * (g >> 1) + (g & 1);
 
     while (pos < end) {
-        while (pos >= base + chunks) { base += chunks; ++s; chunks = shape(s, sp, nch, tiles); }
-        const long long rel = pos - base, item = rel / nch;
-        const int a0 = static_cast<int>(rel - item * nch);
-        const int a1 = end - pos < nch - a0 ? a0 + static_cast<int>(end - pos) : nch;
+        while (pos >= base + units) { base += units; ++s; units = look(s); }
+        const long long rel = pos - base;
+        // the item, its chunks a0 .. a1 - 1 that are this part, its parts and the team that has the first of them
+        const int of = TEAM > 1 && aligned ? pieces(nch) : nch;  // units of an item
+        const long long item = rel / of, item_begin = base + item * of;
+        const int at = static_cast<int>(rel - item * of);
+        int a0 = at, a1 = end - pos < nch - at ? at + static_cast<int>(end - pos) : nch;
+        if (TEAM > 1 && aligned) {
+            const int each = (nch + of - 1) / of;
+            a0 = at * each < nch ? at * each : nch;
+            a1 = a0 + each < nch ? a0 + each : nch;
+        }
+        const long long first_team = item_begin / share;
+        const int parts = static_cast<int>((item_begin + of - 1) / share - first_team) + 1;
+        const long long slot = 2 * team + (pos == begin ? 0 : 1);
         const int h = static_cast<int>(item / tiles), tile = static_cast<int>(item - static_cast<long long>(h) * tiles);
         const int rows_left = sp.n * p.G - tile * 16, rows = rows_left < 16 ? rows_left : 16;
-        const long long item_begin = base + item * nch;
 
         // ------------------------------------------------------------ copies
         const int count = a1 - a0 - member <= 0 ? 0 : (a1 - a0 - member + TEAM - 1) / TEAM;     // this warp's chunks
@@ -216,7 +270,6 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         auto issue = [&](int k, int place) {
             if (k < count) {
                 const int st = k % STAGES, key0 = (a0 + member + k * TEAM) * CH;
-                if (lane < (SMALL ? 4 : 1)) places[warp][st][lane] = place;
                 const int64_t off = (static_cast<int64_t>(place < 0 ? 0 : place) << cv.page_shift) * D + lane * 16;
                 const uint32_t dst = ring + st * CHUNK_BYTES + crow * D;
                 const bool full = key0 + CH <= sp.len && (SMALL ? __all_sync(0xffffffffu, place >= 0 || lane >= slots) : place >= 0);
@@ -250,29 +303,22 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             }
             commit();
         };
-        auto load_exps = [&](int k, int& ek, int& ev) {  // of the places of the k-th chunk
+        auto load_exps = [&](int place, int& ek, int& ev) {
             ek = ev = 0;
-            if (k < count && (!SMALL || lane < slots)) {
-                const int place = places[warp][k % STAGES][SMALL ? lane : 0];
-                if (place >= 0) {
-                    ek = cv.k_exp[place];
-                    ev = cv.v_exp[place];
-                }
+            if (place >= 0) {
+                ek = cv.k_exp[place];
+                ev = cv.v_exp[place];
             }
         };
-        {
-            int id = load_place(0);
+        int place[STAGES];                               // of the chunk at hand and those in the ring behind it
+        place[0] = load_place(0);
 #pragma unroll
-            for (int k = 0; k < STAGES - 1; ++k) {
-                const int next = load_place(k + 1);
-                issue(k, id);
-                id = next;
-            }
+        for (int k = 0; k < STAGES - 1; ++k) {
+            place[k + 1] = load_place(k + 1);
+            issue(k, place[k]);
         }
-        int place_next = load_place(STAGES - 1);
-        __syncwarp();
         int ek_next, ev_next;
-        load_exps(0, ek_next, ev_next);
+        load_exps(place[0], ek_next, ev_next);
 
         // ------------------------------------------------------------ queries: half precision, a power of two taken out of each row
         // Slice 4 x + w of the contraction: a lane's features 16 (t + 4 x) + 4 w .. + 3, the ones that it reads of a key
@@ -337,11 +383,14 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             const int st = k % STAGES, key0 = (a0 + member + k * TEAM) * CH;
             wait_groups<STAGES - 2>();
             __syncwarp();
-            const int ek = ek_next, ev = ev_next;
             // bit j: slot j has no page
-            const int bad = SMALL ? __ballot_sync(0xffffffffu, lane < slots && places[warp][st][lane & 3] < 0) : places[warp][st][0] < 0;
-            issue(k + STAGES - 1, place_next);           // (into the stage that every lane had read before this chunk's barrier)
-            place_next = load_place(k + STAGES);
+            const int bad = SMALL ? __ballot_sync(0xffffffffu, lane < slots && place[0] < 0) : place[0] < 0;
+            const int ek = ek_next, ev = ev_next;
+            issue(k + STAGES - 1, place[STAGES - 1]);    // (into the stage that every lane had read before this chunk's barrier)
+            load_exps(place[1], ek_next, ev_next);
+#pragma unroll
+            for (int i = 0; i < STAGES - 1; ++i) place[i] = place[i + 1];
+            place[STAGES - 1] = load_place(k + STAGES);
             const uint32_t ks = ring + st * CHUNK_BYTES, vs = ks + HALF_BYTES;
             // logits, keys as rows: c[i][r]: keys 16 i + krow (0, 1) and 16 i + krow + 2 (2, 3) of the rows 8 r + 2 t and 8 r + 2 t + 1
             float c[NT][RG][4];
@@ -479,7 +528,6 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     }
                 }
             }
-            load_exps(k + 1, ek_next, ev_next);
         }
         wait_groups<0>();
 
@@ -494,9 +542,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) { o[i][r][y] *= inv; o[i][r][2 + y] *= inv; }
             }
-        const bool whole = a0 == 0 && a1 == nch;
-        const long long first_team = item_begin / share, last_team = (item_begin + nch - 1) / share;
-        const long long slot = 2 * team + (pos == begin ? 0 : 1);
+        const bool whole = parts == 1;
         auto finish = [&](int row, int col, float4 v, float lse2) {     // four features of the item's row
             const int flat_row = tile * 16 + row, tok = flat_row / p.G, gh = flat_row - tok * p.G, head = h * p.G + gh;
             uint2 w;
@@ -528,7 +574,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         } else {
             // the team's warps join through the memory of their rings
             __syncthreads();
-            float* parts = reinterpret_cast<float*>(smem);                // [warp][row][D]
+            float* joined = reinterpret_cast<float*>(smem);                // [warp][row][D]
 #pragma unroll
             for (int r = 0; r < RG; ++r)
 #pragma unroll
@@ -536,8 +582,8 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     const int row = 8 * r + 2 * t + y;
 #pragma unroll
                     for (int x = 0; x < PIECES; ++x) {
-                        parts[(warp * 16 + row) * D + 16 * x + g] = o[x][r][y];
-                        parts[(warp * 16 + row) * D + 16 * x + 8 + g] = o[x][r][2 + y];
+                        joined[(warp * 16 + row) * D + 16 * x + g] = o[x][r][y];
+                        joined[(warp * 16 + row) * D + 16 * x + 8 + g] = o[x][r][2 + y];
                     }
                     if (g == 0) warp_lse[warp][row] = lg[r][y];
                 }
@@ -552,7 +598,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 #pragma unroll
                 for (int w = 0; w < WARPS; ++w) {
                     const float a = tc::ex2_approx(warp_lse[w][row] - ref);
-                    const float4 x = *reinterpret_cast<const float4*>(parts + (w * 16 + row) * D + col);
+                    const float4 x = *reinterpret_cast<const float4*>(joined + (w * 16 + row) * D + col);
                     sum += a;
                     v.x += a * x.x; v.y += a * x.y; v.z += a * x.z; v.w += a * x.w;
                 }
@@ -569,7 +615,6 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         if (!whole) {
             __threadfence();
             bool mine;
-            const int parts = static_cast<int>(last_team - first_team) + 1;
             if (TEAM == 1) {
                 __syncwarp();
                 int old = 0;
@@ -588,7 +633,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     const int row = i / (D / 4), col = i % (D / 4) * 4;
                     float ref = -INFINITY, sum = 0.f;
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    constexpr int BATCH = 8;
+                    constexpr int BATCH = 16;            // (parts in flight: each costs a way to L2 and back)
                     for (int j0 = 0; j0 < parts; j0 += BATCH) {
                         float lj[BATCH];
                         float4 x[BATCH];
@@ -625,7 +670,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             }
         }
         if (TEAM > 1) __syncthreads();                   // (the rings' memory is free again)
-        pos += a1 - a0;
+        pos += TEAM > 1 && aligned ? 1 : a1 - a0;
     }
 }
 

@@ -301,7 +301,8 @@ int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream);
  *   cu_seqlens       : [num_seqs + 1] int32: sequence s owns the new tokens cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (its queries, or the
  *                      keys and values to append); may own none.  Tokens behind the last sequence are left alone.
  *   seq_lens         : [num_seqs] int32: tokens of sequence s, the new ones (its last) included
- * All are device memory, caller-owned.  page in {16, 32, 64, 128}, d in {64, 128} (FLAT_ERR_UNSUPPORTED); num_pages * Hkv < 2^31, max_pages * page <= 2^30.  16-byte aligned, the
+ * All are device memory, caller-owned.  page in {16, 32, 64, 128}, d in {64, 128} (FLAT_ERR_UNSUPPORTED); num_pages * Hkv < 2^31, max_pages * page <= 2^30,
+ * num_seqs * Hkv * max_pages * page <= 2^34.  16-byte aligned, the
  * int32 arrays 4-byte.  max_new >= the new tokens of every sequence (it sizes the grid).
  * What the device finds wrong in page_table, cu_seqlens and seq_lens faults nothing: a sequence whose offsets do not lie in
  * 0 .. total, or that has more new tokens than max_new or than its length, or a length beyond max_pages * page, is left out (FLAT_CACHE_BAD_LENGTH in

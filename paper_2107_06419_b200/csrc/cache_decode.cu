@@ -40,7 +40,7 @@ __host__ __device__ constexpr int SMEM_BYTES(int RG) { return WARPS * STAGES(RG)
 constexpr int ALIGN_COST = 5;                                             // chunks
 // Aligned parts have at least this many chunks, one a warp; of a long item more: its parts are joined one after the other, sixteen in
 // flight (0.03 us each), a warp's chunk takes 0.6 us, so P parts of n chunks take about n / (4 P) 0.6 + 0.03 P us, least at P = sqrt(5 n).
-__device__ __forceinline__ int least_part(int n) { return max(WARPS, static_cast<int>(sqrtf(0.2f * n)) + 1); }
+__device__ __forceinline__ unsigned least_part(unsigned n) { return max(WARPS, static_cast<int>(sqrtf(0.2f * n)) + 1); }
 constexpr float WEIGHT_SHIFT = 15.f;                                      // weights are kept as 2^15 w
 
 struct DecodeArgs {
@@ -118,110 +118,73 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     constexpr int NT = CH / 16;                          // logit blocks of sixteen keys
     constexpr int STAGES = flat::STAGES(RG);
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ long long prefix[THREADS + 1];
     __shared__ float warp_lse[WARPS][16];
     __shared__ int last_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int member = TEAM == 1 ? 0 : warp;             // the warp's place in its team
-    const int team = TEAM == 1 ? blockIdx.x * WARPS + warp : blockIdx.x, teams = TEAM == 1 ? gridDim.x * WARPS : gridDim.x;
+    const unsigned team = TEAM == 1 ? blockIdx.x * WARPS + warp : blockIdx.x, teams = TEAM == 1 ? gridDim.x * WARPS : gridDim.x;
     const CacheView& cv = p.c;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    // ---------------------------------------------------------------- the deal
-    auto shape = [&](int s, Span& sp, int& nch, int& tiles) -> long long {      // chunks of all items of a sequence
+    // ---------------------------------------------------------------- the deal: by every warp for itself, a lane a few sequences
+    // (counts of chunks fit 32 bits: the host sees to it)
+    auto shape = [&](int s, Span& sp, int& nch, int& tiles) {             // chunks of all items of a sequence
         nch = tiles = 0;
-        if (!read_span(cv, s, p.total, p.max_new, sp) || sp.n == 0) return 0;
-        const long long rows = static_cast<long long>(sp.n) * p.G;
-        if (rows > p.most_rows) return 0;
-        tiles = static_cast<int>((rows + 15) / 16);
+        if (!read_span(cv, s, p.total, p.max_new, sp) || sp.n == 0) return 0u;
+        const int64_t rows = static_cast<int64_t>(sp.n) * p.G;
+        if (rows > p.most_rows) return 0u;
+        tiles = (static_cast<int>(rows) + 15) / 16;
         nch = (sp.len + CH - 1) / CH;
-        return static_cast<long long>(nch) * tiles * cv.Hkv;
+        return static_cast<unsigned>(nch) * tiles * cv.Hkv;
     };
-    const int per = (cv.num_seqs + THREADS - 1) / THREADS, s_begin = threadIdx.x * per;
-    const int s_end = s_begin + per < cv.num_seqs ? s_begin + per : cv.num_seqs;
+    const int per = (cv.num_seqs + 31) / 32, s_begin = lane * per, s_end = min(s_begin + per, cv.num_seqs);
     int nch, tiles;
     Span sp;
-    long long units = 0, items = 0;
+    unsigned units = 0, items = 0;
+#pragma unroll 4
     for (int s = s_begin; s < s_end; ++s) {
         units += shape(s, sp, nch, tiles);
-        items += static_cast<long long>(tiles) * cv.Hkv;
+        items += tiles * cv.Hkv;
     }
-    auto block_sum = [&](long long v) {                  // (called by every thread)
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        __syncthreads();
-        if (lane == 0) prefix[warp] = v;
-        __syncthreads();
-        long long sum = 0;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) sum += prefix[w];
-        return sum;
-    };
-    const long long chunks_all = block_sum(units);
+    const unsigned chunks_all = __reduce_add_sync(0xffffffffu, units);
     // An equal share of the chunks each.  Where there are less than half as many items as teams, and it costs no team more than ALIGN_COST
     // chunks, every team has a part of one item instead, and an item's parts are alike: a team that goes from one item to the next
     // pays for two (about as long as ALIGN_COST chunks).
-    long long share = (chunks_all + teams - 1) / teams;
-    int aligned = 0;                                     // chunks of a part, at least
-    auto pieces = [&](int n) {                           // parts of an item of n chunks
-        const int c = max(aligned, least_part(n));
+    unsigned share = (chunks_all + teams - 1) / teams;
+    unsigned aligned = 0;                                // chunks of a part, at least
+    auto pieces = [&](unsigned n) {                      // parts of an item of n chunks
+        const unsigned c = max(aligned, least_part(n));
         return (n + c - 1) / c;
     };
+    auto units_of = [&](unsigned chunks) { return TEAM > 1 && aligned ? tiles * cv.Hkv * pieces(nch) : chunks; };
     if (TEAM > 1) {
-        const long long items_all = block_sum(items);
+        const unsigned items_all = __reduce_add_sync(0xffffffffu, items);
         if (2 * items_all <= teams) {
-            const long long c = (chunks_all + teams - items_all - 1) / (teams - items_all);
-            if (c <= share + ALIGN_COST) aligned = static_cast<int>(c);
+            const unsigned c = (chunks_all + teams - items_all - 1) / (teams - items_all);
+            if (c <= share + ALIGN_COST) aligned = c;
         }
         if (aligned) {
             share = 1;
             units = 0;
-            for (int s = s_begin; s < s_end; ++s) {
-                shape(s, sp, nch, tiles);
-                units += static_cast<long long>(tiles) * cv.Hkv * pieces(nch);
-            }
+            for (int s = s_begin; s < s_end; ++s) units += units_of(shape(s, sp, nch, tiles));
         }
     }
-    {   // the sequences' first units
-        long long sum = units;
+    unsigned upto = units;                               // units of this lane's sequences and those before
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += v;
-        }
-        __syncthreads();
-        prefix[threadIdx.x + 1] = sum;
-        if (threadIdx.x == 0) prefix[0] = 0;
-        __syncthreads();
-        long long before = 0;
-        for (int w = 0; w < warp; ++w) before += prefix[32 * (w + 1)];
-        __syncthreads();
-        prefix[threadIdx.x + 1] = sum + before;
-        __syncthreads();
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
     }
-    const long long all = prefix[THREADS];
-    long long pos = team * share;
-    const long long begin = pos, end = pos + share < all ? pos + share : all;
+    const unsigned all = __shfl_sync(0xffffffffu, upto, 31);
+    unsigned pos = team * share;
+    const unsigned begin = pos, end = min(pos + share, all);
     if (TEAM > 1 && pos >= end) return;                  // (the whole CTA)
-    int s = 0;
-    long long base = 0;
-    nch = tiles = 0;
-    units = 0;                                           // now: of sequence s, which begins with unit `base`
-    auto look = [&](int s) {
-        const long long chunks = shape(s, sp, nch, tiles);
-        return TEAM > 1 && aligned ? static_cast<long long>(tiles) * cv.Hkv * pieces(nch) : chunks;
-    };
-    if (pos < end) {
-        int lo = 0, hi = THREADS;                        // the last thread whose sequences begin at or before pos
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (prefix[mid] <= pos) lo = mid; else hi = mid;
-        }
-        s = lo * per;
-        base = prefix[lo];
-        units = look(s);
-    }
+    // the sequence of the first unit: the first lane whose sequences reach beyond it has it
+    const int from = __ffs(__ballot_sync(0xffffffffu, upto > pos)) - 1;
+    int s = from * per;
+    unsigned base = __shfl_sync(0xffffffffu, upto - units, from < 0 ? 0 : from);
+    if (pos < end) units = units_of(shape(s, sp, nch, tiles));            // from here on: of sequence s, which begins with unit `base`
 
     const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * CHUNK_BYTES;
     const int page_mask = cv.page - 1, slots = SMALL ? CH >> cv.page_shift : 1;
@@ -234,22 +197,21 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     const int krow = 4 * (g >> 1) + (g & 1);
 
     while (pos < end) {
-        while (pos >= base + units) { base += units; ++s; units = look(s); }
-        const long long rel = pos - base;
+        while (pos >= base + units) { base += units; ++s; units = units_of(shape(s, sp, nch, tiles)); }
+        const unsigned rel = pos - base;
         // the item, its chunks a0 .. a1 - 1 that are this part, its parts and the team that has the first of them
-        const int of = TEAM > 1 && aligned ? pieces(nch) : nch;  // units of an item
-        const long long item = rel / of, item_begin = base + item * of;
-        const int at = static_cast<int>(rel - item * of);
-        int a0 = at, a1 = end - pos < nch - at ? at + static_cast<int>(end - pos) : nch;
+        const unsigned of = TEAM > 1 && aligned ? pieces(nch) : nch;      // units of an item
+        const unsigned item = rel / of, item_begin = base + item * of, at = rel - item * of;
+        int a0 = at, a1 = min(at + end - pos, static_cast<unsigned>(nch));
         if (TEAM > 1 && aligned) {
             const int each = (nch + of - 1) / of;
-            a0 = at * each < nch ? at * each : nch;
-            a1 = a0 + each < nch ? a0 + each : nch;
+            a0 = min(static_cast<int>(at) * each, nch);
+            a1 = min(a0 + each, nch);
         }
-        const long long first_team = item_begin / share;
-        const int parts = static_cast<int>((item_begin + of - 1) / share - first_team) + 1;
-        const long long slot = 2 * team + (pos == begin ? 0 : 1);
-        const int h = static_cast<int>(item / tiles), tile = static_cast<int>(item - static_cast<long long>(h) * tiles);
+        const unsigned first_team = item_begin / share;
+        const int parts = (item_begin + of - 1) / share - first_team + 1;
+        const int64_t slot = 2 * team + (pos == begin ? 0 : 1);
+        const int h = item / tiles, tile = item - h * tiles;
         const int rows_left = sp.n * p.G - tile * 16, rows = rows_left < 16 ? rows_left : 16;
 
         // ------------------------------------------------------------ copies
@@ -628,7 +590,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             }
             if (mine) {
                 __threadfence();
-                const long long slot0 = 2 * first_team + (item_begin == first_team * share ? 0 : 1);
+                const int64_t slot0 = 2 * static_cast<int64_t>(first_team) + (item_begin == first_team * share ? 0 : 1);
                 for (int i = TEAM == 1 ? lane : threadIdx.x; i < rows * (D / 4); i += 32 * TEAM) {
                     const int row = i / (D / 4), col = i % (D / 4) * 4;
                     float ref = -INFINITY, sum = 0.f;
@@ -643,7 +605,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                             lj[j] = -INFINITY;
                             x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
                             if (j0 + j < parts) {
-                                const long long q = j0 + j == 0 ? slot0 : 2 * (first_team + j0 + j);
+                                const int64_t q = j0 + j == 0 ? slot0 : 2 * static_cast<int64_t>(first_team + j0 + j);
                                 lj[j] = __ldcg(p.part_lse + q * 16 + row);
                                 x[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + (q * 16 + row) * D + col));
                             }

@@ -123,7 +123,8 @@ int validate_cache(const flat_attn_cache_t* c) {
     if (c->num_pages < 1 || c->Hkv < 1 || c->num_seqs < 1 || c->max_pages < 1) return FLAT_ERR_SHAPE;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return FLAT_ERR_UNSUPPORTED;
     if (c->d != 64 && c->d != 128) return FLAT_ERR_UNSUPPORTED;
-    if (c->Hkv > 65535 || static_cast<int64_t>(c->max_pages) * c->page > (1 << 30) || static_cast<int64_t>(c->num_pages) * c->Hkv > 0x7fffffff)
+    if (c->Hkv > 65535 || static_cast<int64_t>(c->max_pages) * c->page > (1 << 30) || static_cast<int64_t>(c->num_pages) * c->Hkv > 0x7fffffff ||
+        static_cast<int64_t>(c->max_pages) * c->page > (1ll << 34) / c->Hkv / c->num_seqs)
         return FLAT_ERR_SHAPE;
     if (!aligned(c->k_cache, 16) || !aligned(c->v_cache, 16) || !aligned(c->page_table, 4) || !aligned(c->cu_seqlens, 4) || !aligned(c->seq_lens, 4) ||
         !aligned(c->status, 4))

@@ -5,10 +5,11 @@
 // rounding.  A scale that is a power of two costs a floating-point format nothing (its relative precision is the same
 // everywhere), and lets a page whose scale grows be requantised without a second rounding, subnormal numbers aside.
 //
-// Bound: device memory, 2 bytes read and 1 written per feature.  A page and head of a sequence is a unit: its new tokens are
-// read once into registers, 32 bytes a thread and pass, reduced, scaled and written.  With one new token a sequence a warp takes the
-// token's keys or values of a head: there the launch and the chain of dependent loads count (offsets, table entry, exponent), and
-// the page that is requantised when its scale grows, eight rows in flight a lane.
+// Bound: device memory, 2 bytes read and 1 written per feature.  The keys (or the values) of a page and head are a unit: one warp
+// reads its new tokens once into registers (32 bytes a lane and pass, up to eight passes in flight; two or four warps for larger pages),
+// reduces, scales and writes them; what a unit waits for is its chain of loads (offsets, table entry, tokens), so that many
+// small units an SM are better than few large ones.  With one new token a sequence a warp takes the token's keys or values of a head; the
+// page that is requantised when its scale grows has eight rows in flight a lane.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
@@ -34,36 +35,48 @@ __device__ __forceinline__ int exponent_for(float top) {
 __device__ __forceinline__ float power_of_two(int e) {   // -126 <= e <= 127
     return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
 }
-// Two bf16 (one word) to two e4m3, times s.  Infinities become NaN.
+// Two bf16 (one word) to two e4m3, times s.  CHECK: infinities (which the conversion would make the largest number) become NaN.
+template <bool CHECK>
 __device__ __forceinline__ uint32_t quantise2(uint32_t w, float s) {
     float a = __uint_as_float(w << 16) * s, b = __uint_as_float(w & 0xffff0000u) * s;
-    if (isinf(a)) a = __int_as_float(0x7fc00000);
-    if (isinf(b)) b = __int_as_float(0x7fc00000);
+    if (CHECK) {
+        if (isinf(a)) a = __int_as_float(0x7fc00000);
+        if (isinf(b)) b = __int_as_float(0x7fc00000);
+    }
     return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ float finite_top2(uint32_t w, float top) {
-    const float a = fabsf(__uint_as_float(w << 16)), b = fabsf(__uint_as_float(w & 0xffff0000u));
-    if (a < INFINITY) top = fmaxf(top, a);               // (false for NaN)
-    if (b < INFINITY) top = fmaxf(top, b);
-    return top;
-}
+template <bool CHECK>
 __device__ __forceinline__ uint4 quantise16(const uint4& a, const uint4& b, float s) {
     uint4 q;
-    q.x = quantise2(a.x, s) | quantise2(a.y, s) << 16;
-    q.y = quantise2(a.z, s) | quantise2(a.w, s) << 16;
-    q.z = quantise2(b.x, s) | quantise2(b.y, s) << 16;
-    q.w = quantise2(b.z, s) | quantise2(b.w, s) << 16;
+    q.x = quantise2<CHECK>(a.x, s) | quantise2<CHECK>(a.y, s) << 16;
+    q.y = quantise2<CHECK>(a.z, s) | quantise2<CHECK>(a.w, s) << 16;
+    q.z = quantise2<CHECK>(b.x, s) | quantise2<CHECK>(b.y, s) << 16;
+    q.w = quantise2<CHECK>(b.z, s) | quantise2<CHECK>(b.w, s) << 16;
     return q;
 }
-__device__ __forceinline__ float finite_top16(const uint4& a, const uint4& b) {
-    float t = finite_top2(a.x, 0.f);
-    t = finite_top2(a.y, t); t = finite_top2(a.z, t); t = finite_top2(a.w, t);
-    t = finite_top2(b.x, t); t = finite_top2(b.y, t); t = finite_top2(b.z, t); t = finite_top2(b.w, t);
-    return t;
+// The largest finite magnitude of bf16 values, two at a time: magnitude bits plus 0x80 are a positive 16-bit number for finite values
+// and a negative one for infinities and NaN.  `top`: the largest so far of each half; `all`: bit 15 or 31 once one is not finite.
+__device__ __forceinline__ void largest(uint32_t w, uint32_t& top, uint32_t& all) {
+    const uint32_t h = (w & 0x7fff7fffu) + 0x00800080u;
+    all |= h;
+    asm("max.s16x2 %0, %0, %1;" : "+r"(top) : "r"(h));
 }
+__device__ __forceinline__ void largest16(const uint4& a, const uint4& b, uint32_t& top, uint32_t& all) {
+    largest(a.x, top, all); largest(a.y, top, all); largest(a.z, top, all); largest(a.w, top, all);
+    largest(b.x, top, all); largest(b.y, top, all); largest(b.z, top, all); largest(b.w, top, all);
+}
+// Over the warp: that magnitude's bits plus 0x80, and 2^30 if a value was not finite (one number for the warps of a unit to compare).
+__device__ __forceinline__ int warp_largest(uint32_t top, uint32_t all) {
+    const int lo = static_cast<int16_t>(top & 0xffffu), hi = static_cast<int>(top) >> 16;
+    return __reduce_max_sync(0xffffffffu, max(lo, hi)) | (__any_sync(0xffffffffu, (all & 0x80008000u) != 0) ? 1 << 30 : 0);
+}
+constexpr uint32_t NOTHING = 0x00800080u;                // (two zeros)
+__device__ __forceinline__ float magnitude(int largest) { return __uint_as_float(static_cast<uint32_t>((largest & 0xffff) - 0x80) << 16); }
+
 // The rows row, row + step, ... below `rows` (sixteen of their values, from `at` on) rounded again to a scale `down` powers of two above
-// theirs.  Eight rows in flight: what this waits for is latency.
-__device__ __forceinline__ void requantise_rows(uint8_t* at, int row, int rows, int step, int width, int down) {
+// theirs.  Eight rows in flight: what this waits for is latency.  (Not
+// inlined: it is rare, and its registers would cost every call half the warps of an SM.)
+__device__ __noinline__ void requantise_rows(uint8_t* at, int row, int rows, int step, int width, int down) {
     const float s = power_of_two(down > 40 ? -40 : -down);       // (448 * 2^-40 is 0 in e4m3, like everything below)
     constexpr int FLIGHT = 8;
     for (; row < rows; row += step * FLIGHT) {
@@ -129,42 +142,48 @@ append_one_kernel(const __grid_constant__ AppendArgs p) {
     const int64_t place = static_cast<int64_t>(page_id) * p.c.Hkv + h;
     uint8_t* exp = (which ? p.c.v_exp : p.c.k_exp) + place;
     const int was = row > 0 ? *exp : 0;
-    float top = finite_top16(a, b);
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const int e = joint_exponent(top, row > 0, was);
+    uint32_t top = NOTHING, all = 0;
+    largest16(a, b, top, all);
+    const int most = warp_largest(top, all);
+    const int e = joint_exponent(magnitude(most), row > 0, was);
     uint8_t* at = (which ? p.c.v : p.c.k) + place * p.c.page * D + 16 * (lane % LANES);
+    if (lane < LANES)
+        *reinterpret_cast<uint4*>(at + row * D) = most >> 30 ? quantise16<true>(a, b, power_of_two(-e)) : quantise16<false>(a, b, power_of_two(-e));
     if (row > 0 && e + 127 > was) requantise_rows(at, lane / LANES, row, 32 / LANES, D, e + 127 - was);
-    if (lane < LANES) *reinterpret_cast<uint4*>(at + row * D) = quantise16(a, b, power_of_two(-e));
     if (lane == 0 && (row == 0 || e + 127 != was)) *exp = static_cast<uint8_t>(e + 127);
 }
 
-// ---------------------------------------------------------------- a page and head a CTA: the first half of its warps takes K, the second V
+// ---------------------------------------------------------------- a page and head, keys or values: a unit of one, two or four warps
+template <int D, int PAGE> struct Unit {
+    static constexpr int PASSES = PAGE * D / 512 < 8 ? PAGE * D / 512 : 8;        // of a warp: sixteen features a lane
+    static constexpr int WARPS = PAGE * D / 512 / PASSES, PER_CTA = 8 / WARPS;
+};
 template <int D, int PAGE>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, Unit<D, PAGE>::PASSES > 4 ? 2 : 3)
 append_kernel(const __grid_constant__ AppendArgs p) {
-    constexpr int WARPS = PAGE * D / 16 / 32 >= 4 ? 4 : PAGE * D / 16 / 32, SIDE = 32 * WARPS;   // per side
-    constexpr int PASSES = PAGE * D / 16 / SIDE, ROWS = SIDE / (D / 16);
-    __shared__ float tops[2][WARPS];
+    using U = Unit<D, PAGE>;
+    constexpr int ROWS = U::WARPS * 32 / (D / 16);       // of a pass
+    __shared__ int tops[8];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int which = threadIdx.x / SIDE, tid = threadIdx.x % SIDE;
-    const unsigned heads = p.c.Hkv, slots = p.slots;
-    const int h = blockIdx.x % heads, slot = blockIdx.x / heads % slots, s = blockIdx.x / heads / slots;
-    Span sp{};
-    if (!read_span(p.c, s, p.total, p.max_new, sp)) return;
+    const int warp = threadIdx.x >> 5, tid = threadIdx.x % (32 * U::WARPS);
+    const unsigned unit = blockIdx.x * U::PER_CTA + warp / U::WARPS, heads = p.c.Hkv, slots = p.slots;
+    const int which = unit & 1, h = (unit >> 1) % heads, slot = (unit >> 1) / heads % slots, s = (unit >> 1) / heads / slots;
+    Span sp{0, 0, 0};
+    bool work = s < p.c.num_seqs && read_span(p.c, s, p.total, p.max_new, sp) && sp.n > 0;
     const int start = sp.len - sp.n, first_page = start / PAGE, index = first_page + slot;
-    if (sp.n == 0 || index * PAGE >= sp.len) return;
-    int page_id;
-    if (!read_page(p.c, s, index, page_id)) return;
-    const int r0 = slot == 0 ? start - first_page * PAGE : 0, r1 = sp.len - index * PAGE < PAGE ? sp.len - index * PAGE : PAGE;
+    int page_id = 0;
+    work = work && index * PAGE < sp.len && read_page(p.c, s, index, page_id);
+    const int r0 = slot == 0 ? start - first_page * PAGE : 0;
+    const int r1 = !work ? 0 : sp.len - index * PAGE < PAGE ? sp.len - index * PAGE : PAGE;
     const int row = tid / (D / 16), col = tid % (D / 16) * 16;
     const __nv_bfloat16* x = p.x[which] + h * p.sh[which] + col;
     const int64_t token0 = sp.q0 + (index * PAGE - start);      // the token of row 0 (if it were new)
-    uint4 a[PASSES], b[PASSES];
-    float top = 0.f;
+    const int64_t place = static_cast<int64_t>(page_id) * p.c.Hkv + h;
+    uint8_t* exp = (which ? p.c.v_exp : p.c.k_exp) + place;
+    uint4 a[U::PASSES], b[U::PASSES];
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
+    for (int i = 0; i < U::PASSES; ++i) {
         const int r = row + i * ROWS;
         a[i] = b[i] = make_uint4(0, 0, 0, 0);
         if (r >= r0 && r < r1) {
@@ -173,25 +192,31 @@ append_kernel(const __grid_constant__ AppendArgs p) {
             b[i] = v[1];
         }
     }
-    uint8_t* exp = (which ? p.c.v_exp : p.c.k_exp) + static_cast<int64_t>(page_id) * p.c.Hkv + h;
-    const int was = r0 > 0 ? *exp : 0;
+    const int was = work && r0 > 0 ? *exp : 0;
+    uint32_t top = NOTHING, all = 0;
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) top = fmaxf(top, finite_top16(a[i], b[i]));
+    for (int i = 0; i < U::PASSES; ++i) largest16(a[i], b[i], top, all);
+    int most = warp_largest(top, all);
+    if (U::WARPS > 1) {
+        if ((threadIdx.x & 31) == 0) tops[warp] = most;
+        __syncthreads();                                 // (and every thread has read the exponent)
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if ((threadIdx.x & 31) == 0) tops[which][tid >> 5] = top;
-    __syncthreads();                                     // (and every thread has read the exponent)
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, tops[which][w]);
-    const int e = joint_exponent(top, r0 > 0, was);
-    uint8_t* at = (which ? p.c.v : p.c.k) + (static_cast<int64_t>(page_id) * p.c.Hkv + h) * PAGE * D + col;
-    if (r0 > 0 && e + 127 > was) requantise_rows(at, row, r0, ROWS, D, e + 127 - was);
+        for (int w = 0; w < U::WARPS; ++w) {
+            const int other = tops[warp / U::WARPS * U::WARPS + w];
+            most = max(most & 0xffff, other & 0xffff) | ((most | other) & 1 << 30);
+        }
+    }
+    if (!work) return;
+    const int e = joint_exponent(magnitude(most), r0 > 0, was);
+    uint8_t* at = (which ? p.c.v : p.c.k) + place * (PAGE * D) + col;
     const float scale = power_of_two(-e);
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
+    for (int i = 0; i < U::PASSES; ++i) {
         const int r = row + i * ROWS;
-        if (r >= r0 && r < r1) *reinterpret_cast<uint4*>(at + r * D) = quantise16(a[i], b[i], scale);
+        if (r >= r0 && r < r1) *reinterpret_cast<uint4*>(at + r * D) = most >> 30 ? quantise16<true>(a[i], b[i], scale) : quantise16<false>(a[i], b[i], scale);
     }
+    // (the new tokens are out of the registers)
+    if (r0 > 0 && e + 127 > was) requantise_rows(at, row, r0, ROWS, D, e + 127 - was);
     if (tid == 0) *exp = static_cast<uint8_t>(e + 127);
 }
 
@@ -210,12 +235,12 @@ int launch_d(const AppendArgs& p, cudaStream_t st) {
         blocks = (static_cast<int64_t>(p.c.num_seqs) * p.c.Hkv * 2 + 3) / 4;
         cfg.blockDim = dim3(128);
     } else {
-        blocks = static_cast<int64_t>(p.c.num_seqs) * p.c.Hkv * p.slots;
-        const int warps = p.c.page * D / 16 / 32;
-        cfg.blockDim = dim3(64 * (warps < 4 ? warps : 4));
+        const int per_cta = p.c.page == 16 ? Unit<D, 16>::PER_CTA : p.c.page == 32 ? Unit<D, 32>::PER_CTA : p.c.page == 64 ? Unit<D, 64>::PER_CTA : Unit<D, 128>::PER_CTA;
+        blocks = (static_cast<int64_t>(p.c.num_seqs) * p.c.Hkv * p.slots * 2 + per_cta - 1) / per_cta;
+        cfg.blockDim = dim3(256);
         kern = p.c.page == 16 ? append_kernel<D, 16> : p.c.page == 32 ? append_kernel<D, 32> : p.c.page == 64 ? append_kernel<D, 64> : append_kernel<D, 128>;
     }
-    if (blocks > 0x1fffffff) return FLAT_ERR_SHAPE;      // (units, four to a CTA, are counted in 32 bits)
+    if (blocks > 0x0fffffff) return FLAT_ERR_SHAPE;      // (units, up to eight to a CTA, are counted in 31 bits)
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
     return cudaLaunchKernelEx(&cfg, kern, p) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA;
 }

@@ -26,8 +26,8 @@ constexpr int ROPE_FLIGHT = 4;                           // units in flight per 
 
 // How a row's units (two 16-byte vectors, or one: ROPE_ODD) lie.
 enum {
-    ROPE_HALF = 0,         // pairs (i, i + r / 2), r / 2 a multiple of the vector: a unit is two vectors r / 2 apart, the rest pass in pairs of vectors
-    ROPE_NEIGHBOURS = 1,   // pairs (2 i, 2 i + 1): a unit is 32 contiguous bytes
+    ROPE_HALF = 0,         // pairs (i, i + r / 2), r / 2 a multiple of the vector: a unit is two vectors r / 2 apart, or (d - r) / 2 where they pass
+    ROPE_NEIGHBOURS = 1,   // pairs (2 i, 2 i + 1): a unit is two vectors d / 2 apart (next to each other they would share sectors: 30 us against 24)
     ROPE_ODD = 2           // pairs (i, i + r / 2) at any even r: a unit is one vector, its partners are read one by one
 };
 
@@ -66,13 +66,16 @@ struct RopeArgs {
     int tile_shift;                                      // log2 of the tokens a CTA takes
 };
 
+// Floats from one token's angles to the next: cosines, as many sines; not a multiple of 32, so that tokens lie in different banks.
+__host__ __device__ inline int angle_stride(int r) { return 2 * ((r / 2 + 3) & ~3) + 2; }
+
 template <typename T, int MODE>
 __global__ void __launch_bounds__(ROPE_THREADS)
 rope_kernel(const __grid_constant__ RopeArgs p) {
     constexpr int V = 16 / sizeof(T), UNIT = MODE == ROPE_ODD ? V : 2 * V;
-    extern __shared__ float angles[];                    // [token][cos: r / 2 | sin: r / 2], as read in vectors
+    extern __shared__ float angles[];                    // [token][cosines | sines]
     const int half = p.r / 2, tile = 1 << p.tile_shift, n0 = blockIdx.x << p.tile_shift, b = blockIdx.y;
-    const int pad = (half + 3) & ~3;                     // (16-byte rows)
+    const int stride = angle_stride(p.r);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int i = threadIdx.x; i < half << p.tile_shift; i += ROPE_THREADS) {
@@ -85,43 +88,51 @@ rope_kernel(const __grid_constant__ RopeArgs p) {
         sincospif(static_cast<float>(static_cast<int32_t>(turns - (quarter << 30))) * 4.656612873077393e-10f, &s, &co);   // 2^-31
         const float cq = quarter & 1 ? -s : co, sq = quarter & 1 ? co : s;
         const float flip = quarter & 2 ? -p.amplitude : p.amplitude;
-        angles[t * 2 * pad + c] = cq * flip;
-        angles[t * 2 * pad + pad + c] = sq * flip * p.sign;
+        angles[t * stride + c] = cq * flip;
+        angles[t * stride + stride / 2 + c] = sq * flip * p.sign;
     }
     __syncthreads();
-    // Units: consecutive ones of a row side by side, then the rows of the tile's tokens, head after head.
-    const int per_row = p.d / UNIT, row_shift = 31 - __clz(per_row), units = (p.heads << p.tile_shift) << row_shift;
-    for (int u0 = threadIdx.x; u0 - static_cast<int>(threadIdx.x) < units; u0 += ROPE_THREADS * ROPE_FLIGHT) {
+    // Units: those of a row side by side, then the tile's tokens, then the heads: as 256 is a multiple of a head's units, a thread
+    // keeps its token and its place in the row, and with them its cosines and sines.
+    const int per_row = p.d / UNIT, row_shift = 31 - __clz(per_row), head_shift = row_shift + p.tile_shift;
+    const int e = threadIdx.x & (per_row - 1), token = threadIdx.x >> row_shift & (tile - 1), n = n0 + token;
+    // the unit's (first) vector, its pairs' place among the angles; where it is not rotated: `at` behind r
+    const bool turned = MODE != ROPE_HALF || e * UNIT < p.r;
+    const int at = MODE == ROPE_HALF && !turned ? p.r + e * V - half : e * V;
+    const int mate = MODE == ROPE_NEIGHBOURS ? p.d / 2 : turned ? half : (p.d - p.r) / 2;         // from the first vector to the second
+    float cs[V], sn[V];                                  // HALF, ODD: of feature at + j; NEIGHBOURS: of the pairs of both vectors
+    {
+        const float *co = angles + token * stride, *si = co + stride / 2;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int f = MODE == ROPE_NEIGHBOURS ? (2 * j < V ? at + 2 * j : at + mate + 2 * j - V) / 2 : MODE == ROPE_ODD && at + j >= half ? at + j - half : at + j;
+            const bool there = f < half;                 // (beyond: never used)
+            cs[j] = there ? co[f] : 0.f;
+            sn[j] = there ? (MODE == ROPE_ODD && at + j < half ? -si[f] : si[f]) : 0.f;
+        }
+    }
+    const int head_step = ROPE_THREADS >> head_shift;
+    for (int h0 = threadIdx.x >> head_shift; h0 - static_cast<int>(threadIdx.x >> head_shift) < p.heads; h0 += head_step * ROPE_FLIGHT) {
         uint4 a[ROPE_FLIGHT], c[ROPE_FLIGHT];
         float partner[MODE == ROPE_ODD ? ROPE_FLIGHT : 1][V];
         T* out[ROPE_FLIGHT];
-        int at[ROPE_FLIGHT], token[ROPE_FLIGHT];
 #pragma unroll
         for (int i = 0; i < ROPE_FLIGHT; ++i) {
-            const int u = u0 + i * ROPE_THREADS, row = u >> row_shift, e = u & (per_row - 1);
-            token[i] = row & (tile - 1);
-            int h = row >> p.tile_shift;
+            int h = h0 + i * head_step;
             out[i] = nullptr;
-            if (u < units && n0 + token[i] < p.N) {
+            if (h < p.heads && n < p.N) {
                 const bool key = h >= p.Hq;
                 if (key) h -= p.Hq;
                 const RopeSide& side = key ? p.k : p.q;
-                const T* x = static_cast<const T*>(side.x) + b * side.xs[0] + h * side.xs[1] + (n0 + token[i]) * side.xs[2];
-                out[i] = static_cast<T*>(side.y) + b * side.ys[0] + h * side.ys[1] + (n0 + token[i]) * side.ys[2];
-                if (MODE == ROPE_HALF) {
-                    at[i] = e * UNIT < p.r ? e * V : e * UNIT;
-                    a[i] = *reinterpret_cast<const uint4*>(x + at[i]);
-                    c[i] = *reinterpret_cast<const uint4*>(x + at[i] + (at[i] < half ? half : V));
-                } else {
-                    at[i] = e * UNIT;
-                    a[i] = *reinterpret_cast<const uint4*>(x + at[i]);
-                    if (MODE == ROPE_NEIGHBOURS) c[i] = *reinterpret_cast<const uint4*>(x + at[i] + V);
-                    if (MODE == ROPE_ODD) {
+                const T* x = static_cast<const T*>(side.x) + b * side.xs[0] + h * side.xs[1] + n * side.xs[2];
+                out[i] = static_cast<T*>(side.y) + b * side.ys[0] + h * side.ys[1] + n * side.ys[2];
+                a[i] = *reinterpret_cast<const uint4*>(x + at);
+                if (MODE != ROPE_ODD) c[i] = *reinterpret_cast<const uint4*>(x + at + mate);
+                if (MODE == ROPE_ODD) {
 #pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            const int f = at[i] + j;
-                            partner[i][j] = f < p.r ? static_cast<float>(x[f < half ? f + half : f - half]) : 0.f;
-                        }
+                    for (int j = 0; j < V; ++j) {
+                        const int f = at + j;
+                        partner[i][j] = f < p.r ? static_cast<float>(x[f < half ? f + half : f - half]) : 0.f;
                     }
                 }
             }
@@ -131,54 +142,42 @@ rope_kernel(const __grid_constant__ RopeArgs p) {
 #pragma unroll
         for (int i = 0; i < ROPE_FLIGHT; ++i) {
             if (!out[i]) continue;
-            const float *co = angles + token[i] * 2 * pad, *si = co + pad;
-            float x1[V];
+            float x1[V], x2[V];
             unpack(a[i], x1, static_cast<const T*>(nullptr));
             if (MODE == ROPE_ODD) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const int f = at[i] + j;
-                    if (f < half) x1[j] = x1[j] * co[f] - partner[i][j] * si[f];
-                    else if (f < p.r) x1[j] = x1[j] * co[f - half] + partner[i][j] * si[f - half];
-                }
-                *reinterpret_cast<uint4*>(out[i] + at[i]) = pack(x1, static_cast<const T*>(nullptr));
+                for (int j = 0; j < V; ++j)
+                    if (at + j < p.r) x1[j] = x1[j] * cs[j] + partner[i][j] * sn[j];
+                *reinterpret_cast<uint4*>(out[i] + at) = pack(x1, static_cast<const T*>(nullptr));
                 continue;
             }
-            float x2[V];
+            if (MODE == ROPE_HALF && !turned) {
+                *reinterpret_cast<uint4*>(out[i] + at) = a[i];
+                *reinterpret_cast<uint4*>(out[i] + at + mate) = c[i];
+                continue;
+            }
             unpack(c[i], x2, static_cast<const T*>(nullptr));
             if (MODE == ROPE_HALF) {
-                if (at[i] < half) {
-                    float y1[V], y2[V];
+                float y1[V], y2[V];
 #pragma unroll
-                    for (int j = 0; j < V; j += 4) {
-                        const float4 cc = *reinterpret_cast<const float4*>(co + at[i] + j), ss = *reinterpret_cast<const float4*>(si + at[i] + j);
-                        const float cv[4] = {cc.x, cc.y, cc.z, cc.w}, sv[4] = {ss.x, ss.y, ss.z, ss.w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            y1[j + k] = x1[j + k] * cv[k] - x2[j + k] * sv[k];
-                            y2[j + k] = x2[j + k] * cv[k] + x1[j + k] * sv[k];
-                        }
-                    }
-                    *reinterpret_cast<uint4*>(out[i] + at[i]) = pack(y1, static_cast<const T*>(nullptr));
-                    *reinterpret_cast<uint4*>(out[i] + at[i] + half) = pack(y2, static_cast<const T*>(nullptr));
-                } else {
-                    *reinterpret_cast<uint4*>(out[i] + at[i]) = a[i];
-                    *reinterpret_cast<uint4*>(out[i] + at[i] + V) = c[i];
+                for (int j = 0; j < V; ++j) {
+                    y1[j] = x1[j] * cs[j] - x2[j] * sn[j];
+                    y2[j] = x2[j] * cs[j] + x1[j] * sn[j];
                 }
+                *reinterpret_cast<uint4*>(out[i] + at) = pack(y1, static_cast<const T*>(nullptr));
+                *reinterpret_cast<uint4*>(out[i] + at + half) = pack(y2, static_cast<const T*>(nullptr));
             } else {
-                auto rotate = [&](float& u, float& v, int pair) {
-                    if (pair >= half) return;
-                    const float cv = co[pair], sv = si[pair], w = u * cv - v * sv;
-                    v = v * cv + u * sv;
-                    u = w;
-                };
 #pragma unroll
-                for (int j = 0; j < V; j += 2) {
-                    rotate(x1[j], x1[j + 1], (at[i] + j) / 2);
-                    rotate(x2[j], x2[j + 1], (at[i] + V + j) / 2);
+                for (int j = 0; j < V; ++j) {            // pairs j of the 2 V features of both vectors
+                    float &u = 2 * j < V ? x1[2 * j % V] : x2[2 * j % V], &v = 2 * j < V ? x1[2 * j % V + 1] : x2[2 * j % V + 1];
+                    if ((2 * j < V ? at + 2 * j : at + mate + 2 * j - V) < p.r) {
+                        const float w = u * cs[j] - v * sn[j];
+                        v = v * cs[j] + u * sn[j];
+                        u = w;
+                    }
                 }
-                *reinterpret_cast<uint4*>(out[i] + at[i]) = pack(x1, static_cast<const T*>(nullptr));
-                *reinterpret_cast<uint4*>(out[i] + at[i] + V) = pack(x2, static_cast<const T*>(nullptr));
+                *reinterpret_cast<uint4*>(out[i] + at) = pack(x1, static_cast<const T*>(nullptr));
+                *reinterpret_cast<uint4*>(out[i] + at + mate) = pack(x2, static_cast<const T*>(nullptr));
             }
         }
     }
@@ -193,11 +192,10 @@ int launch_typed(const RopeArgs& args, bool neighbours, cudaStream_t st) {
     p.tile_shift = 3;
     const int64_t sms = device_sm_count();
     while (p.tile_shift > 0 && (((p.N - 1) >> p.tile_shift) + 1) * static_cast<int64_t>(p.B) < 2 * sms) --p.tile_shift;
-    const int pad = (p.r / 2 + 3) & ~3;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(((p.N - 1) >> p.tile_shift) + 1, p.B);
     cfg.blockDim = dim3(ROPE_THREADS);
-    cfg.dynamicSmemBytes = static_cast<size_t>(2 * pad) * sizeof(float) << p.tile_shift;
+    cfg.dynamicSmemBytes = static_cast<size_t>(angle_stride(p.r)) * sizeof(float) << p.tile_shift;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

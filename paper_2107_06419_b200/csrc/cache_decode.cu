@@ -50,6 +50,7 @@ struct DecodeArgs {
     float* lse;
     long long q_st, q_sh, o_st, o_sh, total;
     int Hq, G, max_new, most_rows, causal;               // sequences with more than most_rows rows are not this kernel's
+    int beside;                                          // launched behind the other kernel of the same call
     float scale_log2e;
     int* counters;                                       // [teams], 0 between launches
     float* part_lse;                                     // [2 teams][16], base 2
@@ -125,7 +126,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     const unsigned team = TEAM == 1 ? blockIdx.x * WARPS + warp : blockIdx.x, teams = TEAM == 1 ? gridDim.x * WARPS : gridDim.x;
     const CacheView& cv = p.c;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // Behind the call's other kernel (cache_prefill.cu), which starts this one after it has waited for what was before and works on other rows:
+    // the two run side by side, and this one waits for it at its end, so that what comes behind this one comes behind both.
+    if (!p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // ---------------------------------------------------------------- the deal: by every warp for itself, a lane a few sequences
     // (counts of chunks fit 32 bits: the host sees to it)
@@ -179,7 +182,10 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     const unsigned all = __shfl_sync(0xffffffffu, upto, 31);
     unsigned pos = team * share;
     const unsigned begin = pos, end = min(pos + share, all);
-    if (TEAM > 1 && pos >= end) return;                  // (the whole CTA)
+    if (TEAM > 1 && pos >= end) {                        // (the whole CTA)
+        if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
     // the sequence of the first unit: the first lane whose sequences reach beyond it has it
     const int from = __ffs(__ballot_sync(0xffffffffu, upto > pos)) - 1;
     int s = from * per;
@@ -634,6 +640,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         if (TEAM > 1) __syncthreads();                   // (the rings' memory is free again)
         pos += TEAM > 1 && aligned ? 1 : a1 - a0;
     }
+    if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 }  // namespace
@@ -665,11 +672,11 @@ int launch_form(const DecodeArgs& p, bool by_warp, cudaStream_t st) {
 }
 }  // namespace
 
-size_t cache_workspace_bytes(int d) {
-    return counter_bytes() + 2 * most_teams() * 16 * sizeof(float) + 2 * most_teams() * 16 * d * sizeof(float);
+size_t cache_decode_workspace_bytes(int d) {
+    return (counter_bytes() + 2 * most_teams() * 16 * (d + 1) * sizeof(float) + 255) & ~size_t(255);
 }
 
-int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int most_rows, cudaStream_t st) {
+int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int most_rows, bool beside, cudaStream_t st) {
     DecodeArgs p{};
     p.c = cache_view(c);
     p.Q = static_cast<const __nv_bfloat16*>(q.Q);
@@ -678,6 +685,7 @@ int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_pa
     p.q_st = q.q_stride_t; p.q_sh = q.q_stride_h; p.o_st = q.o_stride_t; p.o_sh = q.o_stride_h;
     p.total = q.total;
     p.Hq = q.Hq; p.G = q.Hq / c.Hkv; p.max_new = q.max_new; p.most_rows = most_rows; p.causal = q.causal;
+    p.beside = beside;
     p.scale_log2e = q.scale * 1.4426950408889634f;
     char* w = static_cast<char*>(q.workspace);
     p.counters = reinterpret_cast<int*>(w);

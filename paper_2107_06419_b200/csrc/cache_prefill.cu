@@ -36,7 +36,7 @@ namespace {
 
 constexpr int BM = 128, BN = 64, THREADS = 512;
 constexpr int KS = 3, VS = 3, LS = 3;                    // stages: half-precision keys, values; pages as they come
-constexpr int POLY_LANE = 3;                             // element index mod 4 that takes the polynomial
+constexpr int POLY_LANE = 3;                             // element index mod 8 that takes the polynomial
 // Weights at the reference maximum are 2^9: 64 of them add up to half of MOST_SUM, so that a step passes it only where the reference is
 // exceeded, and what half precision rounds away lies 2^34 below the reference.
 constexpr float SHIFT = 9.f, MOST_SUM = 60000.f;
@@ -82,7 +82,7 @@ __device__ __forceinline__ float exp_store(const uint32_t (&s)[BN], float unit, 
             unpack2(fma2(pack2(__uint_as_float(s[c * 32 + i]), __uint_as_float(s[c * 32 + i + 1])), unit2, neg_m2), p[i], p[i + 1]);
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            p[i] = !TAIL && (i & 3) == POLY_LANE ? ex2_poly(p[i]) : ex2_approx(p[i]);
+            p[i] = !TAIL && (i & 7) == POLY_LANE ? ex2_poly(p[i]) : ex2_approx(p[i]);
             if (TAIL && (c * 32 + i >= nvalid || (out >> (2 * c + i / 16) & 1))) p[i] = 0.f;
         }
 #pragma unroll
@@ -128,9 +128,39 @@ struct PrefillArgs {
     __nv_bfloat16* O;
     float* lse;
     long long q_st, q_sh, o_st, o_sh, total;
-    int Hq, G, max_new, least_rows, causal, slabs;       // sequences of at most least_rows rows are not this kernel's
+    int Hq, G, max_new, least_rows, causal;              // sequences of at most least_rows rows are not this kernel's
     float scale_log2e;
+    int sms, most_items;                                 // CTAs that run at a time; items that the grid was made for
+    int* counters;                                       // [sms][8], 0 between launches
+    float* part_lse;                                     // [sms][2 BM], base 2
+    float* part_o;                                       // [sms][D / 4][2 BM][4]
 };
+
+// One row of an item (place `in` of its 256) from its parts: their normalised outputs and log-sums.
+template <int D>
+__device__ __forceinline__ void join_rows(const PrefillArgs& p, int slot0, int parts, int in, bool there, int token, int head) {
+    const float* lse = p.part_lse + slot0 * 2 * BM + in;
+    float top = -INFINITY, sum = 0.f;
+    for (int i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(lse + i * 2 * BM));
+    const float ref = top == -INFINITY ? 0.f : top;
+    for (int i = 0; i < parts; ++i) sum += ex2_approx(__ldcg(lse + i * 2 * BM) - ref);
+    const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
+    if (p.lse && there) p.lse[static_cast<int64_t>(token) * p.Hq + head] = (sum > 0.f ? ref + log2f(sum) : sum == sum ? -INFINITY : sum) * 0.6931471805599453f;
+    __nv_bfloat16* out = p.O + token * p.o_st + head * p.o_sh;
+    const float4* from = reinterpret_cast<const float4*>(p.part_o) + static_cast<int64_t>(slot0) * (D / 4) * 2 * BM + in;
+#pragma unroll 2
+    for (int c = 0; c < D / 8; ++c) {
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+#pragma unroll 4
+        for (int i = 0; i < parts; ++i) {
+            const float w = ex2_approx(__ldcg(lse + i * 2 * BM) - ref) * inv;
+            const float4 x = __ldcg(from + (static_cast<int64_t>(i) * (D / 4) + 2 * c) * 2 * BM), y = __ldcg(from + (static_cast<int64_t>(i) * (D / 4) + 2 * c + 1) * 2 * BM);
+            a.x += w * x.x; a.y += w * x.y; a.z += w * x.z; a.w += w * x.w;
+            b.x += w * y.x; b.y += w * y.y; b.z += w * y.z; b.w += w * y.w;
+        }
+        if (there) *reinterpret_cast<uint4*>(out + 8 * c) = make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y), pack_bf16x2(b.z, b.w));
+    }
+}
 
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -143,22 +173,53 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + LY::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     __shared__ int top_exp[2], any_bad;
+    // an item in parts: the part's place in the workspace (-1: the item is in one part), its index among them, their number, the item's place
+    __shared__ int part_slot, part_index, part_count, part_item;
     const int warp = warp_index(), lane = threadIdx.x & 31;
     const CacheView& cv = p.c;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // (the previous kernels of the stream have finished before the next one may start: a decode launch behind this one relies on it)
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // the last slabs (under the causal mask the longest) of all sequences and heads first
-    const unsigned heads = cv.Hkv, per_slab = heads * cv.num_seqs;
-    const int slab = p.slabs - 1 - static_cast<int>(blockIdx.x / per_slab), s = blockIdx.x % per_slab / heads, h = blockIdx.x % heads;
+    // ---------------------------------------------------------------- the CTA's work (every warp for itself)
+    // Items: sequence after sequence, their last slabs (under the causal mask the longest) first, the heads side by side.  Those of the last
+    // round, fewer than there are SMs, are split along the keys into as many parts as find an SM.
+    auto slabs_of = [&](int s, Span& sp) {
+        if (!read_span(cv, s, p.total, p.max_new, sp)) return 0;
+        const int rows = sp.n * p.G;
+        return rows <= p.least_rows ? 0 : (rows + 2 * BM - 1) / (2 * BM);
+    };
+    const int per = (cv.num_seqs + 31) / 32, s_end = min(lane * per + per, cv.num_seqs);
     Span sp;
-    if (!read_span(cv, s, p.total, p.max_new, sp)) return;               // (the whole CTA)
-    const int rows = sp.n * p.G, row0 = slab * 2 * BM;
-    if (rows <= p.least_rows || row0 >= rows) return;
-    // keys that any row of the slab sees
+    int upto = 0;                                        // items of this lane's sequences and those before
+    for (int s = lane * per; s < s_end; ++s) upto += slabs_of(s, sp) * cv.Hkv;
+    const int mine_all = upto;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    const int items = __shfl_sync(0xffffffffu, upto, 31), rest = items % p.sms, whole = items - rest;
+    const int split = rest ? min(p.sms / rest, 16) : 1, unit = blockIdx.x;
+    if (unit >= whole + rest * split) return;            // (the whole CTA)
+    if (items > p.most_items) {                          // (offsets that go back and forth: more rows than the tensors have)
+        if (cv.status && threadIdx.x == 0) atomicExch(cv.status, FLAT_CACHE_BAD_LENGTH);
+        return;
+    }
+    const int item = unit < whole ? unit : whole + (unit - whole) / split, part = unit < whole ? 0 : (unit - whole) % split;
+    const int from = __ffs(__ballot_sync(0xffffffffu, upto > item)) - 1;
+    int s = from * per, first = __shfl_sync(0xffffffffu, upto - mine_all, from);
+    int slabs = slabs_of(s, sp);
+    while (item >= first + slabs * cv.Hkv) { first += slabs * cv.Hkv; ++s; slabs = slabs_of(s, sp); }
+    const int h = (item - first) % cv.Hkv, row0 = (slabs - 1 - (item - first) / cv.Hkv) * 2 * BM, rows = sp.n * p.G;
+    // keys that any row of the slab sees; the part's steps j0 .. j0 + nsteps - 1
     const int last_tok = (row0 + 2 * BM < rows ? row0 + 2 * BM - 1 : rows - 1) / p.G;
     const int n = p.causal ? last_tok + 1 + sp.len - sp.n : sp.len;
-    const int nsteps = (n + BN - 1) / BN, pages = (n + cv.page - 1) >> cv.page_shift;
+    const int all_steps = (n + BN - 1) / BN, pages = (n + cv.page - 1) >> cv.page_shift;
+    // (joining costs about a step a part, so n steps take n / P + P in P parts: no more than sqrt(n) of them, of four steps at least)
+    const int parts = unit < whole ? 1 : max(1, min(min(split, all_steps / 4), static_cast<int>(sqrtf(static_cast<float>(all_steps)))));
+    if (part >= parts) return;
+    const int j0 = all_steps * part / parts, nsteps = all_steps * (part + 1) / parts - j0;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < LY::NUM_BARS; ++i)
@@ -166,6 +227,10 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                                 : (i >= LY::K_EMPTY && i < LY::V_FULL) || (i >= LY::V_EMPTY && i < LY::S_FULL) ? 2 : 1);
         *abort_flag = 0;
         top_exp[0] = top_exp[1] = any_bad = 0;
+        part_slot = parts > 1 ? unit - whole : -1;
+        part_index = part;
+        part_count = parts;
+        part_item = (unit - whole) / split;
         fence_mbar_init();
     }
     if (warp == 0) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
@@ -205,7 +270,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         auto load_ids = [&](int j, int (&id)[2]) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int key = j * BN + r0 + 32 * i;
+                const int key = (j0 + j) * BN + r0 + 32 * i;
                 id[i] = -1;
                 if (j < nsteps && key < sp.len) {
                     id[i] = cv.table[static_cast<int64_t>(s) * cv.max_pages + (key >> cv.page_shift)];
@@ -218,7 +283,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                 const uint32_t dst = raw + (j % LS) * 2 * RAW_BYTES;
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) {
-                    const int key = j * BN + r0 + 32 * (i & 1);
+                    const int key = (j0 + j) * BN + r0 + 32 * (i & 1);
                     const int64_t src = ((((static_cast<int64_t>(id[i & 1] < 0 ? 0 : id[i & 1]) * cv.Hkv + h) << cv.page_shift) + (key & (cv.page - 1))) * D)
                                         + 64 * (i >> 1) + 16 * part;
                     const int bytes = id[i & 1] >= 0 ? 16 : 0;
@@ -386,7 +451,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             tmem_ld_x32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
             tmem_ld_x32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
             tc_wait_ld();
-            const int col0 = j * BN;
+            const int col0 = (j0 + j) * BN;
             int out = 0;                                 // (rare) groups of sixteen keys whose page is missing
             if (missing)
                 for (int i = 0; i < BN / 16; ++i) {
@@ -440,26 +505,45 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         if (ok) ok = warp_wait(my_bars + 64 + 8 * ((nsteps - 1) & 1), ((nsteps - 1) >> 1) & 1, abort_s, cv.status, 0xb34 + t);
         if (ok) {
             const float inv = l > 0.f ? two_to(EV - 127 - LIFT) / l : l == l ? 0.f : l;
-            if (p.lse && row < rows)
-                p.lse[static_cast<int64_t>(sp.q0 + tok) * p.Hq + head] = l > 0.f ? (m_ref - SHIFT + log2f(l)) * 0.6931471805599453f : l == l ? -INFINITY : l;
+            const float lse2 = l > 0.f ? m_ref - SHIFT + log2f(l) : l == l ? -INFINITY : l;
+            const int slot = part_slot;
+            if (slot >= 0) p.part_lse[(slot * 2 + t) * BM + mine] = lse2;
+            else if (p.lse && row < rows) p.lse[static_cast<int64_t>(sp.q0 + tok) * p.Hq + head] = lse2 * 0.6931471805599453f;
             tc_fence_after();
             __nv_bfloat16* orow = p.O + (sp.q0 + tok) * p.o_st + head * p.o_sh;
+            float4* prow = reinterpret_cast<float4*>(p.part_o) + (static_cast<int64_t>(slot) * (D / 4) * 2 + t) * BM + mine;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t r[32];
                 tmem_ld_x32(tl + O_COL(t) + c * 32, r);
                 tc_wait_ld();
-                if (row < rows) {
+                float f[32];
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        uint4 w;
-                        w.x = pack_bf16x2(__uint_as_float(r[8 * v + 0]) * inv, __uint_as_float(r[8 * v + 1]) * inv);
-                        w.y = pack_bf16x2(__uint_as_float(r[8 * v + 2]) * inv, __uint_as_float(r[8 * v + 3]) * inv);
-                        w.z = pack_bf16x2(__uint_as_float(r[8 * v + 4]) * inv, __uint_as_float(r[8 * v + 5]) * inv);
-                        w.w = pack_bf16x2(__uint_as_float(r[8 * v + 6]) * inv, __uint_as_float(r[8 * v + 7]) * inv);
-                        *reinterpret_cast<uint4*>(orow + c * 32 + v * 8) = w;
-                    }
+                for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]) * inv;
+                if (slot >= 0) {
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) prow[(c * 8 + v) * 2 * BM] = make_float4(f[4 * v], f[4 * v + 1], f[4 * v + 2], f[4 * v + 3]);
+                } else if (row < rows) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        *reinterpret_cast<uint4*>(orow + c * 32 + v * 8) = make_uint4(pack_bf16x2(f[8 * v], f[8 * v + 1]), pack_bf16x2(f[8 * v + 2], f[8 * v + 3]),
+                                                                                      pack_bf16x2(f[8 * v + 4], f[8 * v + 5]), pack_bf16x2(f[8 * v + 6], f[8 * v + 7]));
                 }
+            }
+        }
+        if (part_slot >= 0) {
+            // -------------------------------------------------------- an item in parts: the warp that comes last with its 32 rows joins them
+            // (in the order of the keys; a part whose waits gave up counts too, so that the counter ends at 0: what it left is not valid, as
+            // `status` says.  Here, in the branch of these warps: the others have given up the registers.)
+            __threadfence();
+            __syncwarp();
+            int* counter = p.counters + part_item * 8 + warp;
+            int last = 0;
+            if (lane == 0) last = atomicAdd(counter, 1) == part_count - 1;
+            if (__shfl_sync(0xffffffffu, last, 0)) {
+                __threadfence();
+                if (lane == 0) *counter = 0;
+                join_rows<D>(p, part_slot - part_index, part_count, t * BM + mine, row < rows, sp.q0 + tok, head);
             }
         }
     }
@@ -470,8 +554,15 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
 
 template <int D>
 int launch_d(const flat_attn_cache_t& c, const PrefillArgs& p, cudaStream_t st) {
+    PrefillArgs args = p;
     if (!ensure_dynamic_smem<cache_prefill_kernel<D>>(Layout<D>::SMEM_BYTES)) return FLAT_ERR_CUDA;
-    const int64_t items = static_cast<int64_t>(p.slabs) * c.num_seqs * c.Hkv;
+    // No more items than this: a sequence has a slab for every 256 rows and one for the rest, and only those with more than least_rows
+    // rows count.  (CTAs without work leave at once, but one after the other.)
+    const int64_t rows = p.total * p.G, slabs = (static_cast<int64_t>(p.max_new) * p.G + 2 * BM - 1) / (2 * BM);
+    const int64_t last = rows / (p.least_rows + 1) < c.num_seqs ? rows / (p.least_rows + 1) : c.num_seqs;
+    const int64_t bound = rows / (2 * BM) + last, most = slabs * c.num_seqs < bound ? slabs * c.num_seqs : bound;
+    args.most_items = static_cast<int>(most * c.Hkv < 0x7fffffff ? most * c.Hkv : 0x7fffffff);
+    const int64_t items = most * c.Hkv + p.sms;          // (parts beyond whole items: fewer than there are SMs)
     if (items > 0x7fffffff) return FLAT_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(items));
@@ -483,12 +574,15 @@ int launch_d(const flat_attn_cache_t& c, const PrefillArgs& p, cudaStream_t st) 
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, cache_prefill_kernel<D>, p) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, cache_prefill_kernel<D>, args) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA;
 }
 
 }  // namespace
 
-int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int least_rows, cudaStream_t st) {
+static size_t prefill_counter_bytes() { return (device_sm_count() * 8 * sizeof(int) + 255) & ~size_t(255); }
+size_t cache_prefill_workspace_bytes(int d) { return prefill_counter_bytes() + static_cast<size_t>(device_sm_count()) * 2 * BM * (d + 1) * sizeof(float); }
+
+int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int least_rows, void* workspace, cudaStream_t st) {
     PrefillArgs p{};
     p.c = cache_view(c);
     p.Q = static_cast<const __nv_bfloat16*>(q.Q);
@@ -497,8 +591,12 @@ int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_p
     p.q_st = q.q_stride_t; p.q_sh = q.q_stride_h; p.o_st = q.o_stride_t; p.o_sh = q.o_stride_h;
     p.total = q.total;
     p.Hq = q.Hq; p.G = q.Hq / c.Hkv; p.max_new = q.max_new; p.least_rows = least_rows; p.causal = q.causal;
+    p.sms = device_sm_count();
+    char* w = static_cast<char*>(workspace);
+    p.counters = reinterpret_cast<int*>(w);
+    p.part_lse = reinterpret_cast<float*>(w + prefill_counter_bytes());
+    p.part_o = p.part_lse + static_cast<size_t>(p.sms) * 2 * BM;
     p.scale_log2e = q.scale * 1.4426950408889634f;
-    p.slabs = static_cast<int>((static_cast<int64_t>(q.max_new) * p.G + 2 * BM - 1) / (2 * BM));
     return c.d == 64 ? launch_d<64>(c, p, st) : launch_d<128>(c, p, st);
 }
 

@@ -614,7 +614,7 @@ int flat_attn_cache_append(const flat_attn_cache_t* c, const void* K, const void
 
 size_t flat_attn_cache_workspace_bytes(int Hq, int Hkv, int d) {
     if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || (d != 64 && d != 128)) return 0;
-    return flat::cache_workspace_bytes(d);
+    return flat::cache_decode_workspace_bytes(d) + flat::cache_prefill_workspace_bytes(d);
 }
 
 int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_params_t* p, void* stream) {
@@ -627,7 +627,8 @@ int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_pa
     const long long in[2] = {p->q_stride_t, p->q_stride_h}, out[2] = {p->o_stride_t, p->o_stride_h}, size[2] = {p->total, p->Hq};
     if (!strides_ok(in, 2, 8) || !strides_ok(out, 2, 8) || !apart(out, size, 2, c->d)) return FLAT_ERR_SHAPE;
     if (!aligned16(p->Q) || !aligned16(p->O) || !aligned(p->workspace, 256) || !aligned(p->lse, 4)) return FLAT_ERR_ALIGN;
-    if (p->workspace_bytes < flat::cache_workspace_bytes(c->d)) return FLAT_ERR_WORKSPACE;
+    const size_t behind = flat::cache_decode_workspace_bytes(c->d);
+    if (p->workspace_bytes < behind + flat::cache_prefill_workspace_bytes(c->d)) return FLAT_ERR_WORKSPACE;
     flat_attn_cache_t q = *c;
     q.status = status_or_library_word(c->status);
     // Rows of a sequence and key head (new tokens times heads a group): up to FEW the warp-level products, whose tiles have sixteen
@@ -638,12 +639,12 @@ int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_pa
     const bool many = static_cast<int64_t>(p->max_new) * (p->Hq / c->Hkv) > FEW, few = !many || c->num_seqs > 1;
     int launches = 0;
     if (many) {
-        const int r = flat::launch_cache_prefill(q, *p, few ? FEW : 0, st);
+        const int r = flat::launch_cache_prefill(q, *p, few ? FEW : 0, static_cast<char*>(p->workspace) + behind, st);
         if (r != FLAT_OK) return r;
         ++launches;
     }
     if (few) {
-        const int r = flat::launch_cache_decode(q, *p, FEW, st);
+        const int r = flat::launch_cache_decode(q, *p, FEW, many, st);
         if (r != FLAT_OK) return r;
         ++launches;
     }

@@ -22,7 +22,7 @@ namespace flat {
 namespace {
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_FLIGHT = 4;                           // units in flight per thread
+constexpr int ROPE_FLIGHT = 2;                           // units in flight per thread (four, and three CTAs an SM: the same; four in two CTAs: 26 us against 22)
 
 // How a row's units (two 16-byte vectors, or one: ROPE_ODD) lie.
 enum {
@@ -70,7 +70,7 @@ struct RopeArgs {
 __host__ __device__ inline int angle_stride(int r) { return 2 * ((r / 2 + 3) & ~3) + 2; }
 
 template <typename T, int MODE>
-__global__ void __launch_bounds__(ROPE_THREADS)
+__global__ void __launch_bounds__(ROPE_THREADS, 4)
 rope_kernel(const __grid_constant__ RopeArgs p) {
     constexpr int V = 16 / sizeof(T), UNIT = MODE == ROPE_ODD ? V : 2 * V;
     extern __shared__ float angles[];                    // [token][cosines | sines]

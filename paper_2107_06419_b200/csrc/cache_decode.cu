@@ -34,6 +34,9 @@ namespace {
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int HALF_BYTES = 4096, CHUNK_BYTES = 2 * HALF_BYTES;            // a chunk's keys, then its values
 // RG: row groups of eight in a tile.  One: three CTAs an SM and two chunks a warp in the ring; two need the registers of two CTAs.
+// (Four, with the queries in shared memory: 48 items of 28 rows 98 us, in two tiles of sixteen 100; its 1,100 instructions a chunk are
+// too long a chain for eight warps an SM.)
+constexpr int TILE = 16;
 __host__ __device__ constexpr int CTAS(int RG) { return RG == 1 ? 3 : 2; }
 __host__ __device__ constexpr int STAGES(int RG) { return RG == 1 ? 2 : 3; }
 __host__ __device__ constexpr int SMEM_BYTES(int RG) { return WARPS * STAGES(RG) * CHUNK_BYTES; }
@@ -118,8 +121,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     constexpr int PIECES = D / 16, RPI = 32 / PIECES;    // 16-byte pieces of a row; rows that a copy instruction brings
     constexpr int NT = CH / 16;                          // logit blocks of sixteen keys
     constexpr int STAGES = flat::STAGES(RG);
+    constexpr int JOIN = D + 4;                          // floats from row to row where the warps join: eight lanes' rows in eight banks' distance
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ float warp_lse[WARPS][16];
+    __shared__ float warp_lse[WARPS][TILE];
     __shared__ int last_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int member = TEAM == 1 ? 0 : warp;             // the warp's place in its team
@@ -137,7 +141,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         if (!read_span(cv, s, p.total, p.max_new, sp) || sp.n == 0) return 0u;
         const int64_t rows = static_cast<int64_t>(sp.n) * p.G;
         if (rows > p.most_rows) return 0u;
-        tiles = (static_cast<int>(rows) + 15) / 16;
+        tiles = (static_cast<int>(rows) + TILE - 1) / TILE;
         nch = (sp.len + CH - 1) / CH;
         return static_cast<unsigned>(nch) * tiles * cv.Hkv;
     };
@@ -207,18 +211,24 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         const unsigned rel = pos - base;
         // the item, its chunks a0 .. a1 - 1 that are this part, its parts and the team that has the first of them
         const unsigned of = TEAM > 1 && aligned ? pieces(nch) : nch;      // units of an item
-        const unsigned item = rel / of, item_begin = base + item * of, at = rel - item * of;
+        const unsigned item = of == 1 ? rel : rel / of, item_begin = base + item * of, at = rel - item * of;
         int a0 = at, a1 = min(at + end - pos, static_cast<unsigned>(nch));
         if (TEAM > 1 && aligned) {
             const int each = (nch + of - 1) / of;
             a0 = min(static_cast<int>(at) * each, nch);
             a1 = min(a0 + each, nch);
         }
-        const unsigned first_team = item_begin / share;
-        const int parts = (item_begin + of - 1) / share - first_team + 1;
+        const unsigned first_team = share == 1 ? item_begin : item_begin / share;
+        const int parts = share == 1 ? of : (item_begin + of - 1) / share - first_team + 1;
         const int64_t slot = 2 * team + (pos == begin ? 0 : 1);
-        const int h = item / tiles, tile = item - h * tiles;
-        const int rows_left = sp.n * p.G - tile * 16, rows = rows_left < 16 ? rows_left : 16;
+        const int h = tiles == 1 ? item : item / tiles, tile = item - h * tiles;
+        const int rows = min(sp.n * p.G - tile * TILE, TILE);
+        // of the item's row: its token and its head of the group
+        auto place_of = [&](int row, int& tok, int& gh) {
+            const int flat = tile * TILE + row;
+            tok = sp.n == 1 ? 0 : flat / p.G;
+            gh = flat - tok * p.G;
+        };
 
         // ------------------------------------------------------------ copies
         const int count = a1 - a0 - member <= 0 ? 0 : (a1 - a0 - member + TEAM - 1) / TEAM;     // this warp's chunks
@@ -295,7 +305,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         int nrow[RG][2];
 #pragma unroll
         for (int r = 0; r < RG; ++r) {
-            const int row = g + 8 * r, flat_row = tile * 16 + row, tok = flat_row / p.G, gh = flat_row - tok * p.G;
+            const int row = g + 8 * r;
+            int tok, gh;
+            place_of(row, tok, gh);
             uint4 raw[D / 64][2];
             float top = 0.f;
 #pragma unroll
@@ -331,7 +343,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     qb[4 * x + w][r][1] = pack_half2(__uint_as_float(hi << 16) * up, __uint_as_float(hi & 0xffff0000u) * up);
                 }
         }
-        const long long lim0 = static_cast<long long>(tile * 16 / p.G) + 1 + sp.len - sp.n;     // keys that every row sees
+        int tok0, gh0;
+        place_of(0, tok0, gh0);
+        const long long lim0 = static_cast<long long>(tok0) + 1 + sp.len - sp.n;     // keys that every row sees
         const int nmin = p.causal && lim0 < sp.len ? static_cast<int>(lim0) : sp.len;
 
         // ------------------------------------------------------------ the chunks
@@ -360,6 +374,29 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             for (int i = 0; i < STAGES - 1; ++i) place[i] = place[i + 1];
             place[STAGES - 1] = load_place(k + STAGES);
             const uint32_t ks = ring + st * CHUNK_BYTES, vs = ks + HALF_BYTES;
+            // base-2 logits; keys that a row does not see take no part
+            const bool masked = key0 + CH > nmin || bad != 0;
+            float uk[NT], wv[NT];                        // of sixteen keys: their scale; what their weights are multiplied by for their values' scale
+            int evs[NT], e_top = -1000;
+            const float ek_scale = two_to(ek - 127);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                uk[i] = SMALL ? __shfl_sync(0xffffffffu, ek_scale, (i * 16) >> cv.page_shift) : ek_scale;
+                evs[i] = SMALL ? __shfl_sync(0xffffffffu, ev, (i * 16) >> cv.page_shift) : ev;
+                e_top = max(e_top, evs[i]);
+            }
+            if (e_top > E) {
+                const float down = E < -500 ? 0.f : two_to(E - e_top);
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+                    for (int r = 0; r < RG; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[i][r][e] *= down;
+                E = e_top;
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) wv[i] = two_to(evs[i] - E);
             // logits, keys as rows: c[i][r]: keys 16 i + krow (0, 1) and 16 i + krow + 2 (2, 3) of the rows 8 r + 2 t and 8 r + 2 t + 1
             float c[NT][RG][4];
 #pragma unroll
@@ -385,33 +422,10 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     }
                 }
             }
-            // base-2 logits; keys that a row does not see take no part
-            const bool masked = key0 + CH > nmin || bad != 0;
-            float uk[NT], wv[NT];                        // of sixteen keys: their scale; what their weights are multiplied by for their values' scale
-            int evs[NT], e_top = -1000;
-            const float ek_scale = two_to(ek - 127);
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                uk[i] = SMALL ? __shfl_sync(0xffffffffu, ek_scale, (i * 16) >> cv.page_shift) : ek_scale;
-                evs[i] = SMALL ? __shfl_sync(0xffffffffu, ev, (i * 16) >> cv.page_shift) : ev;
-                e_top = max(e_top, evs[i]);
-            }
-            if (e_top > E) {
-                const float down = E < -500 ? 0.f : two_to(E - e_top);
-#pragma unroll
-                for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-                    for (int r = 0; r < RG; ++r)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[i][r][e] *= down;
-                E = e_top;
-            }
-#pragma unroll
-            for (int i = 0; i < NT; ++i) wv[i] = two_to(evs[i] - E);
             bool grown = false;
             float mx[RG][2];
 #pragma unroll
-            for (int r = 0; r < RG; ++r)
+            for (int r = 0; r < RG; ++r) {
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -420,22 +434,18 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                         c[i][r][y] *= u;
                         c[i][r][2 + y] *= u;
                     }
-            if (masked) {
+                if (masked) {
 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    const int key = key0 + i * 16 + krow;
-                    const bool gone = bad >> (SMALL ? (i * 16) >> cv.page_shift : 0) & 1;
-#pragma unroll
-                    for (int r = 0; r < RG; ++r)
+                    for (int i = 0; i < NT; ++i) {
+                        const int key = key0 + i * 16 + krow;
+                        const bool gone = bad >> (SMALL ? (i * 16) >> cv.page_shift : 0) & 1;
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
                             if (gone || key >= nrow[r][y]) c[i][r][y] = -INFINITY;
                             if (gone || key + 2 >= nrow[r][y]) c[i][r][2 + y] = -INFINITY;
                         }
+                    }
                 }
-            }
-#pragma unroll
-            for (int r = 0; r < RG; ++r)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     mx[r][y] = fmaxf(c[0][r][y], c[0][r][2 + y]);
@@ -443,10 +453,11 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     for (int i = 1; i < NT; ++i) mx[r][y] = tc::max3(mx[r][y], c[i][r][y], c[i][r][2 + y]);
                     grown = grown || mx[r][y] > m[r][y];
                 }
+            }
             // (the maximum is taken over the lanes only where one of them has met a larger logit)
             if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-                for (int r = 0; r < RG; ++r)
+                for (int r = 0; r < RG; ++r) {
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const float mn = fmaxf(m[r][y], column_max(mx[r][y]));
@@ -456,8 +467,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 #pragma unroll
                         for (int i = 0; i < PIECES; ++i) { o[i][r][y] *= a; o[i][r][2 + y] *= a; }
                     }
+                }
             }
-            uint32_t pb[NT][RG][2];                      // weights as the right operand
+            uint32_t pb[NT][RG][2];                 // weights as the right operand
 #pragma unroll
             for (int r = 0; r < RG; ++r) {
 #pragma unroll
@@ -488,11 +500,13 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     ldsm_bytes(vs + row * D + (D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3)) * 16, b);
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        uint32_t a[4];                   // rows g, g + 8: features 16 (x + y) + g, + 8
+                        uint32_t a[4];               // rows g, g + 8: features 16 (x + y) + g, + 8
                         halves(b[2 * y], a[0], a[2]);
                         halves(b[2 * y + 1], a[1], a[3]);
 #pragma unroll
-                        for (int r = 0; r < RG; ++r) mma16(o[x + y][r], a, pb[i][r][0], pb[i][r][1]);
+                        for (int r = 0; r < RG; ++r) {
+                            mma16(o[x + y][r], a, pb[i][r][0], pb[i][r][1]);
+                        }
                     }
                 }
             }
@@ -512,7 +526,9 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             }
         const bool whole = parts == 1;
         auto finish = [&](int row, int col, float4 v, float lse2) {     // four features of the item's row
-            const int flat_row = tile * 16 + row, tok = flat_row / p.G, gh = flat_row - tok * p.G, head = h * p.G + gh;
+            int tok, gh;
+            place_of(row, tok, gh);
+            const int head = h * p.G + gh;
             uint2 w;
             w.x = tc::pack_bf16x2(v.x, v.y);
             w.y = tc::pack_bf16x2(v.z, v.w);
@@ -526,9 +542,11 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                 for (int y = 0; y < 2; ++y) {
                     const int row = 8 * r + 2 * t + y;
                     if (row >= rows) continue;
-                    const int flat_row = tile * 16 + row, tok = flat_row / p.G, head = h * p.G + flat_row - tok * p.G;
+                    int tok, gh;
+                    place_of(row, tok, gh);
+                    const int head = h * p.G + gh;
                     __nv_bfloat16* out = p.O + (sp.q0 + tok) * p.o_st + head * p.o_sh + g;
-                    float* part = p.part_o + (slot * 16 + row) * D + g;
+                    float* part = p.part_o + (slot * TILE + row) * D + g;
 #pragma unroll
                     for (int x = 0; x < PIECES; ++x)
 #pragma unroll
@@ -536,13 +554,13 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                             if (whole) out[16 * x + 8 * e] = __float2bfloat16(o[x][r][2 * e + y]);
                             else part[16 * x + 8 * e] = o[x][r][2 * e + y];
                         }
-                    if (g == 0 && !whole) p.part_lse[slot * 16 + row] = lg[r][y];
+                    if (g == 0 && !whole) p.part_lse[slot * TILE + row] = lg[r][y];
                     if (g == 0 && whole && p.lse) p.lse[static_cast<long long>(sp.q0 + tok) * p.Hq + head] = lg[r][y] * 0.6931471805599453f;
                 }
         } else {
             // the team's warps join through the memory of their rings
             __syncthreads();
-            float* joined = reinterpret_cast<float*>(smem);                // [warp][row][D]
+            float* joined = reinterpret_cast<float*>(smem);                // [warp][row][JOIN]
 #pragma unroll
             for (int r = 0; r < RG; ++r)
 #pragma unroll
@@ -550,8 +568,8 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     const int row = 8 * r + 2 * t + y;
 #pragma unroll
                     for (int x = 0; x < PIECES; ++x) {
-                        joined[(warp * 16 + row) * D + 16 * x + g] = o[x][r][y];
-                        joined[(warp * 16 + row) * D + 16 * x + 8 + g] = o[x][r][2 + y];
+                        joined[(warp * 8 * RG + row) * JOIN + 16 * x + g] = o[x][r][y];
+                        joined[(warp * 8 * RG + row) * JOIN + 16 * x + 8 + g] = o[x][r][2 + y];
                     }
                     if (g == 0) warp_lse[warp][row] = lg[r][y];
                 }
@@ -566,7 +584,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 #pragma unroll
                 for (int w = 0; w < WARPS; ++w) {
                     const float a = tc::ex2_approx(warp_lse[w][row] - ref);
-                    const float4 x = *reinterpret_cast<const float4*>(joined + (w * 16 + row) * D + col);
+                    const float4 x = *reinterpret_cast<const float4*>(joined + (w * 8 * RG + row) * JOIN + col);
                     sum += a;
                     v.x += a * x.x; v.y += a * x.y; v.z += a * x.z; v.w += a * x.w;
                 }
@@ -574,28 +592,34 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                 v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
                 if (whole) finish(row, col, v, lse2);
                 else {
-                    *reinterpret_cast<float4*>(p.part_o + (slot * 16 + row) * D + col) = v;
-                    if (col == 0) p.part_lse[slot * 16 + row] = lse2;
+                    *reinterpret_cast<float4*>(p.part_o + (slot * TILE + row) * D + col) = v;
+                    if (col == 0) p.part_lse[slot * TILE + row] = lse2;
                 }
             }
         }
         // ------------------------------------------------------------ an item in several teams: the last one joins its parts
         if (!whole) {
-            __threadfence();
+            // (one thread's fences, with the barriers on either side, order what all of them have written and will read)
             bool mine;
+            auto arrive = [&] {
+                __threadfence();
+                const bool last = atomicAdd(p.counters + first_team, 1) == parts - 1;
+                __threadfence();
+                return last;
+            };
             if (TEAM == 1) {
                 __syncwarp();
-                int old = 0;
-                if (lane == 0) old = atomicAdd(p.counters + first_team, 1);
-                mine = __shfl_sync(0xffffffffu, old, 0) == parts - 1;
+                int last = 0;
+                if (lane == 0) last = arrive();
+                mine = __shfl_sync(0xffffffffu, last, 0);
+                __syncwarp();
             } else {
                 __syncthreads();
-                if (threadIdx.x == 0) last_word = atomicAdd(p.counters + first_team, 1) == parts - 1;
+                if (threadIdx.x == 0) last_word = arrive();
                 __syncthreads();
                 mine = last_word;
             }
             if (mine) {
-                __threadfence();
                 const int64_t slot0 = 2 * static_cast<int64_t>(first_team) + (item_begin == first_team * share ? 0 : 1);
                 for (int i = TEAM == 1 ? lane : threadIdx.x; i < rows * (D / 4); i += 32 * TEAM) {
                     const int row = i / (D / 4), col = i % (D / 4) * 4;
@@ -612,8 +636,8 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                             x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
                             if (j0 + j < parts) {
                                 const int64_t q = j0 + j == 0 ? slot0 : 2 * static_cast<int64_t>(first_team + j0 + j);
-                                lj[j] = __ldcg(p.part_lse + q * 16 + row);
-                                x[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + (q * 16 + row) * D + col));
+                                lj[j] = __ldcg(p.part_lse + q * TILE + row);
+                                x[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + (q * TILE + row) * D + col));
                             }
                         }
 #pragma unroll
@@ -647,6 +671,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 
 namespace {
 size_t most_teams() { return static_cast<size_t>(device_sm_count()) * 3 * WARPS; }     // (three CTAs an SM, a team a warp)
+size_t most_part_rows() { return static_cast<size_t>(device_sm_count()) * 3 * WARPS * 2 * TILE; }    // (two places a team)
 size_t counter_bytes() { return (most_teams() * sizeof(int) + 255) & ~size_t(255); }
 
 template <int D, int RG, int TEAM, bool SMALL>
@@ -673,7 +698,7 @@ int launch_form(const DecodeArgs& p, bool by_warp, cudaStream_t st) {
 }  // namespace
 
 size_t cache_decode_workspace_bytes(int d) {
-    return (counter_bytes() + 2 * most_teams() * 16 * (d + 1) * sizeof(float) + 255) & ~size_t(255);
+    return (counter_bytes() + most_part_rows() * (d + 1) * sizeof(float) + 255) & ~size_t(255);
 }
 
 int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int most_rows, bool beside, cudaStream_t st) {
@@ -690,12 +715,12 @@ int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_pa
     char* w = static_cast<char*>(q.workspace);
     p.counters = reinterpret_cast<int*>(w);
     p.part_lse = reinterpret_cast<float*>(w + counter_bytes());
-    p.part_o = p.part_lse + 2 * most_teams() * 16;
+    p.part_o = p.part_lse + most_part_rows();
     const int64_t rows = static_cast<int64_t>(q.max_new) * p.G, most = rows < most_rows ? rows : most_rows;
-    const int64_t items = static_cast<int64_t>(c.num_seqs) * c.Hkv * ((most + 15) / 16);
+    const int64_t items = static_cast<int64_t>(c.num_seqs) * c.Hkv * ((most + TILE - 1) / TILE);
     const bool by_warp = items >= static_cast<int64_t>(most_teams());
-    if (c.d == 64) return rows <= 8 ? launch_form<64, 1>(p, by_warp, st) : launch_form<64, 2>(p, by_warp, st);
-    return rows <= 8 ? launch_form<128, 1>(p, by_warp, st) : launch_form<128, 2>(p, by_warp, st);
+    if (c.d == 64) return most <= 8 ? launch_form<64, 1>(p, by_warp, st) : launch_form<64, 2>(p, by_warp, st);
+    return most <= 8 ? launch_form<128, 1>(p, by_warp, st) : launch_form<128, 2>(p, by_warp, st);
 }
 
 }  // namespace flat

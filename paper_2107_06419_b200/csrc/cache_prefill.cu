@@ -35,7 +35,7 @@ using namespace tc;
 namespace {
 
 constexpr int BM = 128, BN = 64, THREADS = 512;
-constexpr int KS = 3, VS = 3, LS = 3;                    // stages: half-precision keys, values; pages as they come
+constexpr int KS = 3, VS = 3;                            // stages of half-precision keys and values
 constexpr int POLY_LANE = 3;                             // element index mod 8 that takes the polynomial
 // Weights at the reference maximum are 2^9: 64 of them add up to half of MOST_SUM, so that a step passes it only where the reference is
 // exceeded, and what half precision rounds away lies 2^34 below the reference.
@@ -46,10 +46,13 @@ __host__ __device__ constexpr uint32_t S_COL(int t, int b) { return 128u * t + 6
 __host__ __device__ constexpr uint32_t O_COL(int t) { return 256u + 128u * t; }
 
 template <int D> struct Layout {
+    static constexpr int LS = D == 128 ? 4 : 6;          // steps of pages on their way
     static constexpr int Q_BYTES = BM * D * 2, KV_BYTES = BN * D * 2, RAW_BYTES = BN * D;
     static constexpr int K_AT = 2 * Q_BYTES, V_AT = K_AT + KS * KV_BYTES, RAW_AT = V_AT + VS * KV_BYTES, BARS_AT = RAW_AT + LS * 2 * RAW_BYTES;
     static constexpr int Q_FULL = 0, K_FULL = 2, K_EMPTY = K_FULL + KS, V_FULL = K_EMPTY + KS, V_EMPTY = V_FULL + VS, S_FULL = V_EMPTY + VS,
-                         P_FULL = S_FULL + 4, PV_DONE = P_FULL + 4, NUM_BARS = PV_DONE + 4;
+                         P_FULL = S_FULL + 4, PV_DONE = P_FULL + 4,
+                         EXPS_READY = PV_DONE + 4, SCALE_FULL = EXPS_READY + 1, RAW_FULL = SCALE_FULL + 2, SCALE_EMPTY = RAW_FULL + LS,
+                         RAW_EMPTY = SCALE_EMPTY + 2, NUM_BARS = RAW_EMPTY + LS;
     static constexpr int SMEM_BYTES = BARS_AT + NUM_BARS * 8 + 32 + 1024;
     static_assert(SMEM_BYTES <= 232448, "shared memory");
 };
@@ -108,18 +111,27 @@ __device__ __forceinline__ float row_max(const uint32_t (&s)[BN], float unit, in
     return m;
 }
 
-// Sixteen e4m3 (a piece) times a half-precision pair `by`, as two 16-byte chunks.
-__device__ __forceinline__ void widen16(const uint4& v, __half2 by, uint32_t (&h)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// Sixteen e4m3 (a piece) times a half-precision pair `by`.
+__device__ __forceinline__ void widen16(const uint32_t (&w)[4], __half2 by, uint32_t (&h)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
-        const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&r), by);
-        h[i] = *reinterpret_cast<const uint32_t*>(&x);
+    for (int i = 0; i < 4; ++i) {
+        uint32_t lo, hi;
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w[i]));
+        const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&lo), by), y = __hmul2(*reinterpret_cast<const __half2*>(&hi), by);
+        h[2 * i] = *reinterpret_cast<const uint32_t*>(&x);
+        h[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&y);
     }
 }
 __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ void lds16(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// `bytes` (a multiple of 16, like both addresses) to shared memory of this CTA; they count on the mbarrier.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
 struct PrefillArgs {
@@ -162,11 +174,18 @@ __device__ __forceinline__ void join_rows(const PrefillArgs& p, int slot0, int p
     }
 }
 
+// What a CTA works on: sequence, its first query, length, tokens before the new ones; head; rows of the sequence and the slab's first;
+// keys that the slab sees; the part's steps; whether the second tile has rows.
+struct Work {
+    int s, q0, len, before, h, rows, row0, n, j0, nsteps, two;
+};
+constexpr int GROUPS = 32;                               // groups of sixteen tokens that are looked up at a time: eight steps
+
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
 cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     using LY = Layout<D>;
-    constexpr int Q_BYTES = LY::Q_BYTES, KV_BYTES = LY::KV_BYTES, RAW_BYTES = LY::RAW_BYTES;
+    constexpr int Q_BYTES = LY::Q_BYTES, KV_BYTES = LY::KV_BYTES, RAW_BYTES = LY::RAW_BYTES, LS = LY::LS;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bars = reinterpret_cast<uint64_t*>(base + LY::BARS_AT);
@@ -175,6 +194,8 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     __shared__ int top_exp[2], any_bad;
     // an item in parts: the part's place in the workspace (-1: the item is in one part), its index among them, their number, the item's place
     __shared__ int part_slot, part_index, part_count, part_item;
+    __shared__ Work work;                                // (what the roles need of the mapping below: read again, not kept in registers)
+    __shared__ int scales[2 * GROUPS];                   // of sixteen tokens: the exponents of the keys and values, a byte each; -1: no page there
     const int warp = warp_index(), lane = threadIdx.x & 31;
     const CacheView& cv = p.c;
     // (the previous kernels of the stream have finished before the next one may start: a decode launch behind this one relies on it)
@@ -189,172 +210,208 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         const int rows = sp.n * p.G;
         return rows <= p.least_rows ? 0 : (rows + 2 * BM - 1) / (2 * BM);
     };
+    {
     const int per = (cv.num_seqs + 31) / 32, s_end = min(lane * per + per, cv.num_seqs);
-    Span sp;
-    int upto = 0;                                        // items of this lane's sequences and those before
-    for (int s = lane * per; s < s_end; ++s) upto += slabs_of(s, sp) * cv.Hkv;
-    const int mine_all = upto;
+    auto before = [&](int v) {                           // of the lanes below and this one
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += v;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += u;
+        }
+        return v;
+    };
+    Span sp;
+    int mine_all = 0;                                    // of this lane's sequences: items, and then units
+    long long steps_all = 0;
+    for (int s = lane * per; s < s_end; ++s) {
+        const int n = slabs_of(s, sp) * cv.Hkv;
+        mine_all += n;
+        steps_all += static_cast<long long>(n) * ((sp.len + BN - 1) / BN);
     }
-    const int items = __shfl_sync(0xffffffffu, upto, 31), rest = items % p.sms, whole = items - rest;
-    const int split = rest ? min(p.sms / rest, 16) : 1, unit = blockIdx.x;
-    if (unit >= whole + rest * split) return;            // (the whole CTA)
+    const int items = __reduce_add_sync(0xffffffffu, mine_all);
     if (items > p.most_items) {                          // (offsets that go back and forth: more rows than the tensors have)
         if (cv.status && threadIdx.x == 0) atomicExch(cv.status, FLAT_CACHE_BAD_LENGTH);
         return;
     }
-    const int item = unit < whole ? unit : whole + (unit - whole) / split, part = unit < whole ? 0 : (unit - whole) % split;
-    const int from = __ffs(__ballot_sync(0xffffffffu, upto > item)) - 1;
+    // All items in one round: parts of `each` steps, as many as there are SMs.  Several rounds: the last one's items in `split` parts each.
+    // Joining costs about a step a part, so n steps take n / P + P in P parts: no more than sqrt(n) of them, of four steps at least.
+    int each = 0;
+    if (items < p.sms) {
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) steps_all += __shfl_xor_sync(0xffffffffu, steps_all, o);
+        each = static_cast<int>((steps_all + p.sms - items - 1) / (p.sms - items));
+    }
+    auto most_parts = [&](int steps, int wanted) { return max(1, min(min(wanted, 16), min(steps / 4, static_cast<int>(sqrtf(static_cast<float>(steps)))))); };
+    auto parts_of = [&](int steps) { return each ? most_parts(steps, (steps + each - 1) / each) : 1; };       // (by the sequence's length)
+    if (each) {
+        mine_all = 0;
+        for (int s = lane * per; s < s_end; ++s) mine_all += slabs_of(s, sp) * cv.Hkv * parts_of((sp.len + BN - 1) / BN);
+    }
+    const int upto = before(mine_all), units = __shfl_sync(0xffffffffu, upto, 31);
+    const int rest = each ? 0 : units % p.sms, whole = units - rest, split = rest ? min(p.sms / rest, 16) : 1, unit = blockIdx.x;
+    if (unit >= whole + rest * split) return;            // (the whole CTA)
+    const int entry = unit < whole ? unit : whole + (unit - whole) / split;      // among the units before the split
+    const int from = __ffs(__ballot_sync(0xffffffffu, upto > entry)) - 1;
     int s = from * per, first = __shfl_sync(0xffffffffu, upto - mine_all, from);
-    int slabs = slabs_of(s, sp);
-    while (item >= first + slabs * cv.Hkv) { first += slabs * cv.Hkv; ++s; slabs = slabs_of(s, sp); }
-    const int h = (item - first) % cv.Hkv, row0 = (slabs - 1 - (item - first) / cv.Hkv) * 2 * BM, rows = sp.n * p.G;
+    int slabs = slabs_of(s, sp), of = parts_of((sp.len + BN - 1) / BN);
+    while (entry >= first + slabs * cv.Hkv * of) {
+        first += slabs * cv.Hkv * of;
+        ++s;
+        slabs = slabs_of(s, sp);
+        of = parts_of((sp.len + BN - 1) / BN);
+    }
+    const int item = (entry - first) / of, h = item % cv.Hkv, row0 = (slabs - 1 - item / cv.Hkv) * 2 * BM, rows = sp.n * p.G;
     // keys that any row of the slab sees; the part's steps j0 .. j0 + nsteps - 1
     const int last_tok = (row0 + 2 * BM < rows ? row0 + 2 * BM - 1 : rows - 1) / p.G;
     const int n = p.causal ? last_tok + 1 + sp.len - sp.n : sp.len;
-    const int all_steps = (n + BN - 1) / BN, pages = (n + cv.page - 1) >> cv.page_shift;
-    // (joining costs about a step a part, so n steps take n / P + P in P parts: no more than sqrt(n) of them, of four steps at least)
-    const int parts = unit < whole ? 1 : max(1, min(min(split, all_steps / 4), static_cast<int>(sqrtf(static_cast<float>(all_steps)))));
+    const int all_steps = (n + BN - 1) / BN;
+    // (an early slab may have fewer steps than its sequence has parts)
+    const int parts = each ? min(of, all_steps) : unit < whole ? 1 : most_parts(all_steps, split);
+    const int part = each ? (entry - first) % of : unit < whole ? 0 : (unit - whole) % split;
     if (part >= parts) return;
-    const int j0 = all_steps * part / parts, nsteps = all_steps * (part + 1) / parts - j0;
-
     if (threadIdx.x == 0) {
+        const int j0 = all_steps * part / parts;
+        work = Work{s, sp.q0, sp.len, sp.len - sp.n, h, rows, row0, n, j0, all_steps * (part + 1) / parts - j0, rows - row0 > BM};
+        part_slot = parts == 1 ? -1 : each ? unit : unit - whole;
+        part_index = part;
+        part_count = parts;
+        part_item = each ? unit - part : (unit - whole) / split;
+    }
+    }
+    if (threadIdx.x == 32) {
         for (int i = 0; i < LY::NUM_BARS; ++i)
-            mbar_init(&bars[i], i < LY::K_EMPTY || (i >= LY::V_FULL && i < LY::V_EMPTY) || (i >= LY::P_FULL && i < LY::PV_DONE) ? 4
+            mbar_init(&bars[i], i == LY::EXPS_READY ? 8
+                                : i < LY::K_EMPTY || (i >= LY::V_FULL && i < LY::V_EMPTY) || (i >= LY::P_FULL && i < LY::PV_DONE) || i >= LY::SCALE_EMPTY ? 4
                                 : (i >= LY::K_EMPTY && i < LY::V_FULL) || (i >= LY::V_EMPTY && i < LY::S_FULL) ? 2 : 1);
         *abort_flag = 0;
         top_exp[0] = top_exp[1] = any_bad = 0;
-        part_slot = parts > 1 ? unit - whole : -1;
-        part_index = part;
-        part_count = parts;
-        part_item = (unit - whole) / split;
         fence_mbar_init();
     }
     if (warp == 0) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    {   // the largest exponents of the keys and values, and whether a page is missing
-        int ke = 0, ve = 0, bad = 0;
-        for (int i = threadIdx.x; i < pages; i += THREADS) {
-            int id;
-            if (read_page(cv, s, i, id)) {
-                const int64_t at = static_cast<int64_t>(id) * cv.Hkv + h;
-                ke = max(ke, static_cast<int>(cv.k_exp[at]));
-                ve = max(ve, static_cast<int>(cv.v_exp[at]));
-            } else {
-                bad = 1;
-            }
-        }
-        ke = __reduce_max_sync(0xffffffffu, ke);
-        ve = __reduce_max_sync(0xffffffffu, ve);
-        bad = __reduce_max_sync(0xffffffffu, bad);
-        if (lane == 0) { atomicMax(&top_exp[0], ke); atomicMax(&top_exp[1], ve); if (bad) any_bad = 1; }
-        __syncthreads();
-    }
-    const int EK = top_exp[0], EV = top_exp[1];
     const uint32_t tmem = *tmem_slot;
     const uint32_t bars_s = smem_u32(bars), abort_s = smem_u32(const_cast<int*>(abort_flag)), base_s = smem_u32(base);
+    const int nsteps = work.nsteps;
 
     if (warp >= 12) {
-        // ------------------------------------------------------------ keys and values: pages -> half-precision tiles
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        const int tid = threadIdx.x - 384;
+        // ------------------------------------------------------------ keys and values: e4m3 pages -> half-precision tiles
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        const int tid = threadIdx.x - 384, u = tid >> 2, q = tid & 3, len = work.len, key0 = work.j0 * BN + u;
         constexpr int PIECES = BN * D / 16 / 128;        // of 16 bytes, a thread and tile: 4 (d = 128) or 2
-        // piece i: sixteen features from 64 (i / 2) + 16 (tid % 4) of the row tid / 4 + 32 (i % 2): eight lanes write to eight banks
-        const uint32_t raw = base_s + LY::RAW_AT + tid * 16;
-        const int r0 = tid >> 2, part = tid & 3;
-        auto load_ids = [&](int j, int (&id)[2]) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int key = (j0 + j) * BN + r0 + 32 * i;
-                id[i] = -1;
-                if (j < nsteps && key < sp.len) {
-                    id[i] = cv.table[static_cast<int64_t>(s) * cv.max_pages + (key >> cv.page_shift)];
-                    if (id[i] < 0 || id[i] >= cv.num_pages) id[i] = -1;
-                }
-            }
+        // Piece i: sixteen features from 16 q on, of panel (i / 2) ^ (u % 2) (of 64 features; d = 64: the only one), of the row u + 32 (i % 2):
+        // eight lanes then read two rows in eight different banks, and write eight.
+        auto panel = [&](int i) { return D == 128 ? (i >> 1) ^ (u & 1) : 0; };
+        const uint32_t chunk0 = ((2 * q) ^ (u & 7)) << 4, chunk1 = ((2 * q + 1) ^ (u & 7)) << 4;
+        bool ok = true;
+        auto wait = [&](int bar, uint32_t parity, int code) {
+            if (ok) ok = warp_wait(bars_s + 8 * bar, parity, abort_s, cv.status, code);
         };
-        auto issue = [&](int j, const int (&id)[2]) {
-            if (j < nsteps) {
-                const uint32_t dst = raw + (j % LS) * 2 * RAW_BYTES;
-#pragma unroll
-                for (int i = 0; i < PIECES; ++i) {
-                    const int key = (j0 + j) * BN + r0 + 32 * (i & 1);
-                    const int64_t src = ((((static_cast<int64_t>(id[i & 1] < 0 ? 0 : id[i & 1]) * cv.Hkv + h) << cv.page_shift) + (key & (cv.page - 1))) * D)
-                                        + 64 * (i >> 1) + 16 * part;
-                    const int bytes = id[i & 1] >= 0 ? 16 : 0;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * 2048), "l"(cv.k + src), "r"(bytes) : "memory");
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + RAW_BYTES + i * 2048), "l"(cv.v + src), "r"(bytes) : "memory");
-                }
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        auto load_exps = [&](const int (&id)[2], int (&e)[4]) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                e[i] = e[2 + i] = 0;
-                if (id[i] >= 0) {
-                    const int64_t at = static_cast<int64_t>(id[i]) * cv.Hkv + h;
-                    e[i] = cv.k_exp[at];
-                    e[2 + i] = cv.v_exp[at];
-                }
-            }
-        };
-        auto convert = [&](uint32_t from, uint32_t to, int e0, int e1, int top) {
+        auto convert = [&](uint32_t (&v)[PIECES][4], uint32_t to, int e0, int e1, int top) {
             // (tokens that no row of the slab sees may lie in pages that the largest was not taken over: they must stay finite)
             const __half2 by[2] = {__float2half2_rn(two_to(min(e0 - top, 0) + LIFT)), __float2half2_rn(two_to(min(e1 - top, 0) + LIFT))};
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                uint4 v;
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from + i * 2048) : "memory");
                 uint32_t x[8];
-                widen16(v, by[i & 1], x);
-                const int row = r0 + 32 * (i & 1);
-                const uint32_t at = to + (i >> 1) * (BN * 128) + row * 128;
-                sts16(at + (((2 * part) ^ (row & 7)) << 4), x[0], x[1], x[2], x[3]);
-                sts16(at + (((2 * part + 1) ^ (row & 7)) << 4), x[4], x[5], x[6], x[7]);
+                widen16(v[i], by[i & 1], x);
+                const uint32_t at = to + panel(i) * (BN * 128) + (u + 32 * (i & 1)) * 128;
+                sts16(at + chunk0, x[0], x[1], x[2], x[3]);
+                sts16(at + chunk1, x[4], x[5], x[6], x[7]);
             }
             fence_proxy_async_smem();
             __syncwarp();
         };
-        // ids of the steps j + 1, j + 2 and exponents of step j are at hand when step j begins
-        int id1[2], id2[2], e[4];
-        bool ok = true;
-        {
-            int id0[2];
-            load_ids(0, id0);
-            load_ids(1, id1);
-            load_ids(2, id2);
-            issue(0, id0);
-            issue(1, id1);
-            load_exps(id0, e);
-        }
+        wait(LY::EXPS_READY, 0, 0xb13);
+        const int EK = top_exp[0], EV = top_exp[1];
         for (int j = 0; j < nsteps && ok; ++j) {
-            int id3[2], next[4];
-            load_ids(j + 3, id3);
-            load_exps(id1, next);
-            asm volatile("cp.async.wait_group %0;" ::"n"(LS - 2) : "memory");
-            issue(j + 2, id2);
-            const uint32_t from = raw + (j % LS) * 2 * RAW_BYTES;
-            ok = warp_wait(bars_s + 8 * (LY::K_EMPTY + j % KS), ((j / KS) & 1) ^ 1, abort_s, cv.status, 0xb10);
+            if (j % 8 == 0) wait(LY::SCALE_FULL + ((j >> 3) & 1), (j >> 4) & 1, 0xb14);
+            wait(LY::RAW_FULL + j % LS, (j / LS) & 1, 0xb12);
             if (!ok) break;
-            convert(from, base_s + LY::K_AT + (j % KS) * KV_BYTES, e[0], e[1], EK);
-            if (lane == 0) mbar_arrive(&bars[LY::K_FULL + j % KS]);
-            ok = warp_wait(bars_s + 8 * (LY::V_EMPTY + j % VS), ((j / VS) & 1) ^ 1, abort_s, cv.status, 0xb11);
-            if (!ok) break;
-            convert(from + RAW_BYTES, base_s + LY::V_AT + (j % VS) * KV_BYTES, e[2], e[3], EV);
-            if (lane == 0) mbar_arrive(&bars[LY::V_FULL + j % VS]);
+            const uint32_t from = base_s + LY::RAW_AT + (j % LS) * 2 * RAW_BYTES + u * D + q * 16;
+            uint32_t k[PIECES][4], v[PIECES][4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) { id1[i] = id2[i]; id2[i] = id3[i]; e[i] = next[i]; e[2 + i] = next[2 + i]; }
+            for (int i = 0; i < PIECES; ++i) {
+                lds16(from + 32 * (i & 1) * D + panel(i) * 64, k[i]);
+                lds16(from + RAW_BYTES + 32 * (i & 1) * D + panel(i) * 64, v[i]);
+            }
+            const int g0 = (j * 4 + (u >> 4)) & (2 * GROUPS - 1), e0 = scales[g0], e1 = scales[g0 + 2];
+            // (rows without a token hold anything: zeros)
+            const bool none0 = e0 < 0 || key0 + j * BN >= len, none1 = e1 < 0 || key0 + j * BN + 32 >= len;
+            if (__any_sync(0xffffffffu, none0 || none1)) {
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i)
+                    if (i & 1 ? none1 : none0) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) k[i][e] = v[i][e] = 0u;
+                    }
+            }
+            wait(LY::K_EMPTY + j % KS, ((j / KS) & 1) ^ 1, 0xb10);
+            if (!ok) break;
+            convert(k, base_s + LY::K_AT + (j % KS) * KV_BYTES, e0 & 255, e1 & 255, EK);
+            if (lane == 0) {
+                mbar_arrive(&bars[LY::K_FULL + j % KS]);
+                mbar_arrive(&bars[LY::RAW_EMPTY + j % LS]);      // (all of it is in registers)
+            }
+            wait(LY::V_EMPTY + j % VS, ((j / VS) & 1) ^ 1, 0xb11);
+            if (!ok) break;
+            convert(v, base_s + LY::V_AT + (j % VS) * KV_BYTES, e0 >> 8 & 255, e1 >> 8 & 255, EV);
+            if (lane == 0) {
+                mbar_arrive(&bars[LY::V_FULL + j % VS]);
+                if (j % 8 == 7) mbar_arrive(&bars[LY::SCALE_EMPTY + ((j >> 3) & 1)]);
+            }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
     } else if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-        if (warp <= 9) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 10) {
+            // -------------------------------------------------------- page table, exponents and copies, eight steps at a time (a lane sixteen tokens)
+            const int32_t* table = cv.table + static_cast<int64_t>(work.s) * cv.max_pages;
+            const int end = min(work.len, (work.j0 + nsteps) * BN);
+            constexpr uint32_t BYTES = 16 * D;           // of sixteen tokens: they lie in one page, one after the other
+            bool ok = true;
+            int issued = 0;
+            auto wait = [&](int bar, uint32_t parity, int code) {
+                if (ok) ok = warp_wait(bars_s + 8 * bar, parity, abort_s, cv.status, code);
+            };
+            auto look = [&](int b) {                     // the lane's sixteen tokens of batch b: page * heads + head; -1: no page there
+                const int key = work.j0 * BN + (b * GROUPS + lane) * 16;
+                if (b * 8 >= nsteps || key >= end) return -1;
+                const int id = table[key >> cv.page_shift];
+                return id >= 0 && id < cv.num_pages ? id * cv.Hkv + work.h : -1;
+            };
+            int next = look(0);
+            for (int b = 0; b * 8 < nsteps && ok; ++b) {
+                const int place = next, key = work.j0 * BN + (b * GROUPS + lane) * 16;
+                const int64_t src = ((static_cast<int64_t>(place < 0 ? 0 : place) << cv.page_shift) + (key & (cv.page - 1))) * D;
+                int scale = -1;
+                if (place >= 0) scale = cv.k_exp[place] | cv.v_exp[place] << 8;
+                next = look(b + 1);
+                for (int i = 0; i < 8 && b * 8 + i < nsteps && ok; ++i) {
+                    const int j = b * 8 + i, st = j % LS;
+                    wait(LY::RAW_EMPTY + st, ((j / LS) & 1) ^ 1, 0xb16);
+                    if (!ok) break;
+                    const unsigned have = __ballot_sync(0xffffffffu, place >= 0) >> (4 * i) & 15;
+                    if (lane == 0) mbar_arrive_expect_tx(&bars[LY::RAW_FULL + st], 2 * BYTES * __popc(have));
+                    __syncwarp();
+                    if (place >= 0 && lane >> 2 == i) {
+                        const uint32_t dst = base_s + LY::RAW_AT + st * 2 * RAW_BYTES + (lane & 3) * BYTES;
+                        bulk_load(dst, cv.k + src, BYTES, bars_s + 8 * (LY::RAW_FULL + st));
+                        bulk_load(dst + RAW_BYTES, cv.v + src, BYTES, bars_s + 8 * (LY::RAW_FULL + st));
+                    }
+                    __syncwarp();
+                    issued = j + 1;
+                    if (i == 0) {                        // (behind the first copies: the exponents have arrived by now)
+                        wait(LY::SCALE_EMPTY + (b & 1), ((b >> 1) & 1) ^ 1, 0xb15);
+                        if (!ok) break;
+                        scales[(b & 1) * GROUPS + lane] = scale;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bars[LY::SCALE_FULL + (b & 1)]);
+                    }
+                }
+            }
+            if (!ok)                                     // (copies in flight end before the CTA does)
+                for (int j = issued > LS ? issued - LS : 0; j < issued; ++j) drain_wait(&bars[LY::RAW_FULL + j % LS], (j / LS) & 1);
+        } else if (warp <= 9) {
             // -------------------------------------------------------- MMA issuer of tile t (whole warp walks, one lane issues)
             const int t = warp - 8;
             constexpr uint32_t IDESC_S = idesc_half(BM, BN, 0), IDESC_PV = idesc_half(BM, D, 1);
@@ -365,6 +422,15 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             auto wait = [&](int bar, uint32_t parity, int code) {
                 if (ok) ok = warp_wait(bars_s + 8 * bar, parity, abort_s, cv.status, code);
             };
+            if (t == 1 && !work.two)                          // (no rows in this tile: only let the stages go)
+                for (int j = 0; j < nsteps && ok; ++j) {
+                    wait(LY::K_FULL + j % KS, (j / KS) & 1, 0xb25);
+                    if (ok && lane == 0) mbar_arrive(&bars[LY::K_EMPTY + j % KS]);
+                    wait(LY::V_FULL + j % VS, (j / VS) & 1, 0xb26);
+                    if (ok && lane == 0) mbar_arrive(&bars[LY::V_EMPTY + j % VS]);
+                    __syncwarp();
+                }
+            else {
             auto issue_s = [&](int j) {                  // S_t(j) = Q_t K_j^T, then release the K stage
                 const uint64_t kd = k_desc + static_cast<uint64_t>(((j % KS) * KV_BYTES) >> 4);
 #pragma unroll
@@ -400,22 +466,50 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                 if (elect_one()) { issue_pv(j); if (more) issue_s(j + 2); }
                 __syncwarp();
             }
+            }
         }
     } else {
         // ------------------------------------------------------------ softmax + epilogue (warps 0-7)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-        const int t = warp >> 2, mine = (warp & 3) * 32 + lane, row = row0 + t * BM + mine;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        const int n = work.n, j0 = work.j0, rows = work.rows;
+        const int32_t* table = cv.table + static_cast<int64_t>(work.s) * cv.max_pages;
+        const int last_page = (min(n, (j0 + nsteps) * BN) - 1) >> cv.page_shift;      // of the part
+        const bool active = warp < 4 || work.two;
+        const int t = warp >> 2, mine = (warp & 3) * 32 + lane, row = work.row0 + t * BM + mine;
         const uint32_t tl = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         const uint32_t my_bars = bars_s + 8 * (LY::S_FULL + 2 * t);       // S_FULL of the tile; P_FULL and PV_DONE 32 and 64 bytes on
-        const int tok = (row < rows ? row : rows - 1) / p.G, head = h * p.G + (row < rows ? row - tok * p.G : 0);
-        float unit;
-        {   // the query row into half precision
-            const uint4* q = reinterpret_cast<const uint4*>(p.Q + (sp.q0 + tok) * p.q_st + head * p.q_sh);
+        const int tok = (row < rows ? row : rows - 1) / p.G, head = work.h * p.G + (row < rows ? row - tok * p.G : 0), token = work.q0 + tok;
+        float unit = 0.f;
+        {
+            const uint4* q = reinterpret_cast<const uint4*>(p.Q + token * p.q_st + head * p.q_sh);
             uint4 v[D / 8];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) v[i] = active && row < rows ? q[i] : make_uint4(0, 0, 0, 0);
+            // the part's largest exponents of the keys and values, and whether a page is missing
+            int ke = 0, ve = 0, bad = 0;
+            for (int i = (j0 * BN >> cv.page_shift) + threadIdx.x; i <= last_page; i += 256) {
+                int id;
+                if (read_page(cv, work.s, i, id)) {
+                    const int place = id * cv.Hkv + work.h;
+                    ke = max(ke, static_cast<int>(cv.k_exp[place]));
+                    ve = max(ve, static_cast<int>(cv.v_exp[place]));
+                } else {
+                    bad = 1;
+                }
+            }
+            ke = __reduce_max_sync(0xffffffffu, ke);
+            ve = __reduce_max_sync(0xffffffffu, ve);
+            bad = __any_sync(0xffffffffu, bad);
+            if (lane == 0) {
+                atomicMax(&top_exp[0], ke);
+                atomicMax(&top_exp[1], ve);
+                if (bad) any_bad = 1;
+                mbar_arrive(&bars[LY::EXPS_READY]);
+            }
+            // the query row into half precision
             float top = 0.f;
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
-                v[i] = row < rows ? q[i] : make_uint4(0, 0, 0, 0);
                 const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u))));
@@ -423,7 +517,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;  // the row's largest: 2^e to 2^(e + 1)
             e = e < -100 ? -100 : e;
             const float up = two_to(14 - e);
-            unit = p.scale_log2e * two_to(e - 14) * two_to(EK - 127 - LIFT);
+            unit = p.scale_log2e * two_to(e - 14);
             const uint32_t at = base_s + t * Q_BYTES + mine * 128;
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
@@ -437,12 +531,14 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars[LY::Q_FULL + t]);
         }
+        bool ok = warp_wait(bars_s + 8 * LY::EXPS_READY, 0, abort_s, cv.status, 0xb35);
+        unit *= two_to(top_exp[0] - 127 - LIFT);
+        if (active) {
         const bool missing = any_bad != 0;
         float m_ref = -INFINITY, l = 0.f;
-        const int nrow = p.causal && tok + 1 + sp.len - sp.n < n ? tok + 1 + sp.len - sp.n : n;
+        const int nrow = p.causal ? min(tok + 1 + work.before, n) : n;
         const int nrow_min = __shfl_sync(0xffffffffu, nrow, 0);
-        bool ok = true;
-        for (int j = 0; j < nsteps; ++j) {
+        for (int j = 0; j < nsteps && ok; ++j) {
             const uint32_t s_addr = tl + S_COL(t, j & 1);
             ok = warp_wait(my_bars + 8 * (j & 1), (j >> 1) & 1, abort_s, cv.status, 0xb30 + t);
             if (!ok) break;
@@ -457,7 +553,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                 for (int i = 0; i < BN / 16; ++i) {
                     const int index = (col0 + 16 * i) >> cv.page_shift;
                     int id = 0;
-                    if (index < pages) id = cv.table[static_cast<int64_t>(s) * cv.max_pages + index];
+                    if (index <= last_page) id = table[index];
                     if (id < 0 || id >= cv.num_pages) out |= 1 << i;
                 }
             const bool tail = col0 + BN > nrow_min || out != 0;          // (warp-uniform) some row has masked keys in this step
@@ -504,13 +600,13 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         }
         if (ok) ok = warp_wait(my_bars + 64 + 8 * ((nsteps - 1) & 1), ((nsteps - 1) >> 1) & 1, abort_s, cv.status, 0xb34 + t);
         if (ok) {
-            const float inv = l > 0.f ? two_to(EV - 127 - LIFT) / l : l == l ? 0.f : l;
+            const float inv = l > 0.f ? two_to(top_exp[1] - 127 - LIFT) / l : l == l ? 0.f : l;
             const float lse2 = l > 0.f ? m_ref - SHIFT + log2f(l) : l == l ? -INFINITY : l;
             const int slot = part_slot;
             if (slot >= 0) p.part_lse[(slot * 2 + t) * BM + mine] = lse2;
-            else if (p.lse && row < rows) p.lse[static_cast<int64_t>(sp.q0 + tok) * p.Hq + head] = lse2 * 0.6931471805599453f;
+            else if (p.lse && row < rows) p.lse[static_cast<int64_t>(token) * p.Hq + head] = lse2 * 0.6931471805599453f;
             tc_fence_after();
-            __nv_bfloat16* orow = p.O + (sp.q0 + tok) * p.o_st + head * p.o_sh;
+            __nv_bfloat16* orow = p.O + token * p.o_st + head * p.o_sh;
             float4* prow = reinterpret_cast<float4*>(p.part_o) + (static_cast<int64_t>(slot) * (D / 4) * 2 + t) * BM + mine;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -543,8 +639,9 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             if (__shfl_sync(0xffffffffu, last, 0)) {
                 __threadfence();
                 if (lane == 0) *counter = 0;
-                join_rows<D>(p, part_slot - part_index, part_count, t * BM + mine, row < rows, sp.q0 + tok, head);
+                join_rows<D>(p, part_slot - part_index, part_count, t * BM + mine, row < rows, token, head);
             }
+        }
         }
     }
     tc_fence_before();

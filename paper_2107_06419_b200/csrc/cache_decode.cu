@@ -146,14 +146,24 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         return static_cast<unsigned>(nch) * tiles * cv.Hkv;
     };
     const int per = (cv.num_seqs + 31) / 32, s_begin = lane * per, s_end = min(s_begin + per, cv.num_seqs);
-    int nch, tiles;
-    Span sp;
+    int nch = 0, tiles = 0;
+    Span sp{0, 0, 0};
     unsigned units = 0, items = 0;
 #pragma unroll 4
     for (int s = s_begin; s < s_end; ++s) {
         units += shape(s, sp, nch, tiles);
         items += tiles * cv.Hkv;
     }
+    // (up to 32 sequences: a lane keeps its one, and what the warp needs of any of them comes by shuffle)
+    const Span own = sp;
+    const int own_nch = nch, own_tiles = tiles;
+    auto fetch = [&](int s) {                            // chunks of all items of sequence s; sp, nch, tiles
+        if (per > 1) return shape(s, sp, nch, tiles);
+        sp = Span{__shfl_sync(0xffffffffu, own.q0, s), __shfl_sync(0xffffffffu, own.n, s), __shfl_sync(0xffffffffu, own.len, s)};
+        nch = __shfl_sync(0xffffffffu, own_nch, s);
+        tiles = __shfl_sync(0xffffffffu, own_tiles, s);
+        return static_cast<unsigned>(nch) * tiles * cv.Hkv;
+    };
     const unsigned chunks_all = __reduce_add_sync(0xffffffffu, units);
     // An equal share of the chunks each.  Where there are less than half as many items as teams, and it costs no team more than ALIGN_COST
     // chunks, every team has a part of one item instead, and an item's parts are alike: a team that goes from one item to the next
@@ -174,7 +184,8 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         if (aligned) {
             share = 1;
             units = 0;
-            for (int s = s_begin; s < s_end; ++s) units += units_of(shape(s, sp, nch, tiles));
+            if (per == 1) units = units_of(0);           // (the lane's own)
+            else for (int s = s_begin; s < s_end; ++s) units += units_of(shape(s, sp, nch, tiles));
         }
     }
     unsigned upto = units;                               // units of this lane's sequences and those before
@@ -194,7 +205,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     const int from = __ffs(__ballot_sync(0xffffffffu, upto > pos)) - 1;
     int s = from * per;
     unsigned base = __shfl_sync(0xffffffffu, upto - units, from < 0 ? 0 : from);
-    if (pos < end) units = units_of(shape(s, sp, nch, tiles));            // from here on: of sequence s, which begins with unit `base`
+    if (pos < end) units = units_of(fetch(s));            // from here on: of sequence s, which begins with unit `base`
 
     const uint32_t ring = ptx::smem_u32(smem) + warp * STAGES * CHUNK_BYTES;
     const int page_mask = cv.page - 1, slots = SMALL ? CH >> cv.page_shift : 1;
@@ -207,7 +218,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     const int krow = 4 * (g >> 1) + (g & 1);
 
     while (pos < end) {
-        while (pos >= base + units) { base += units; ++s; units = units_of(shape(s, sp, nch, tiles)); }
+        while (pos >= base + units) { base += units; ++s; units = units_of(fetch(s)); }
         const unsigned rel = pos - base;
         // the item, its chunks a0 .. a1 - 1 that are this part, its parts and the team that has the first of them
         const unsigned of = TEAM > 1 && aligned ? pieces(nch) : nch;      // units of an item

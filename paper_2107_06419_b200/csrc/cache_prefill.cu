@@ -220,14 +220,22 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         }
         return v;
     };
-    Span sp;
-    int mine_all = 0;                                    // of this lane's sequences: items, and then units
-    long long steps_all = 0;
+    Span sp{0, 0, 0};
+    int mine_all = 0, slabs = 0;                         // of this lane's sequences: items, and then units
+    unsigned steps_all = 0;                              // (used where there are fewer items than SMs: it fits then)
     for (int s = lane * per; s < s_end; ++s) {
-        const int n = slabs_of(s, sp) * cv.Hkv;
-        mine_all += n;
-        steps_all += static_cast<long long>(n) * ((sp.len + BN - 1) / BN);
+        slabs = slabs_of(s, sp);
+        mine_all += slabs * cv.Hkv;
+        steps_all += static_cast<unsigned>(slabs * cv.Hkv) * ((sp.len + BN - 1) / BN);
     }
+    // (up to 32 sequences: a lane keeps its one, and what the warp needs of any of them comes by shuffle)
+    const Span own = sp;
+    const int own_slabs = slabs;
+    auto fetch = [&](int s) {
+        if (per > 1) return slabs_of(s, sp);
+        sp = Span{__shfl_sync(0xffffffffu, own.q0, s), __shfl_sync(0xffffffffu, own.n, s), __shfl_sync(0xffffffffu, own.len, s)};
+        return __shfl_sync(0xffffffffu, own_slabs, s);
+    };
     const int items = __reduce_add_sync(0xffffffffu, mine_all);
     if (items > p.most_items) {                          // (offsets that go back and forth: more rows than the tensors have)
         if (cv.status && threadIdx.x == 0) atomicExch(cv.status, FLAT_CACHE_BAD_LENGTH);
@@ -237,15 +245,17 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     // Joining costs about a step a part, so n steps take n / P + P in P parts: no more than sqrt(n) of them, of four steps at least.
     int each = 0;
     if (items < p.sms) {
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) steps_all += __shfl_xor_sync(0xffffffffu, steps_all, o);
-        each = static_cast<int>((steps_all + p.sms - items - 1) / (p.sms - items));
+        steps_all = __reduce_add_sync(0xffffffffu, steps_all);
+        each = (steps_all + p.sms - items - 1) / static_cast<unsigned>(p.sms - items);
     }
     auto most_parts = [&](int steps, int wanted) { return max(1, min(min(wanted, 16), min(steps / 4, static_cast<int>(sqrtf(static_cast<float>(steps)))))); };
     auto parts_of = [&](int steps) { return each ? most_parts(steps, (steps + each - 1) / each) : 1; };       // (by the sequence's length)
     if (each) {
-        mine_all = 0;
-        for (int s = lane * per; s < s_end; ++s) mine_all += slabs_of(s, sp) * cv.Hkv * parts_of((sp.len + BN - 1) / BN);
+        if (per == 1) mine_all = slabs * cv.Hkv * parts_of((sp.len + BN - 1) / BN);          // (the lane's own)
+        else {
+            mine_all = 0;
+            for (int s = lane * per; s < s_end; ++s) mine_all += slabs_of(s, sp) * cv.Hkv * parts_of((sp.len + BN - 1) / BN);
+        }
     }
     const int upto = before(mine_all), units = __shfl_sync(0xffffffffu, upto, 31);
     const int rest = each ? 0 : units % p.sms, whole = units - rest, split = rest ? min(p.sms / rest, 16) : 1, unit = blockIdx.x;
@@ -253,11 +263,12 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     const int entry = unit < whole ? unit : whole + (unit - whole) / split;      // among the units before the split
     const int from = __ffs(__ballot_sync(0xffffffffu, upto > entry)) - 1;
     int s = from * per, first = __shfl_sync(0xffffffffu, upto - mine_all, from);
-    int slabs = slabs_of(s, sp), of = parts_of((sp.len + BN - 1) / BN);
+    slabs = fetch(s);
+    int of = parts_of((sp.len + BN - 1) / BN);
     while (entry >= first + slabs * cv.Hkv * of) {
         first += slabs * cv.Hkv * of;
         ++s;
-        slabs = slabs_of(s, sp);
+        slabs = fetch(s);
         of = parts_of((sp.len + BN - 1) / BN);
     }
     const int item = (entry - first) / of, h = item % cv.Hkv, row0 = (slabs - 1 - item / cv.Hkv) * 2 * BM, rows = sp.n * p.G;

@@ -631,12 +631,11 @@ int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_pa
     if (p->workspace_bytes < behind + flat::cache_prefill_workspace_bytes(c->d)) return FLAT_ERR_WORKSPACE;
     flat_attn_cache_t q = *c;
     q.status = status_or_library_word(c->status);
-    // Rows of a sequence and key head (new tokens times heads a group): few of them go to the warp-level products, whose tiles have
-    // sixteen rows, more to the tcgen05 form, whose tiles have 128 and which reads the cache once for all of them.  Sixteen is the border where
-    // that form finds two SMs or more for an item to split its keys over, 64 otherwise (even shares of the keys then outweigh reading
-    // them once for every sixteen rows).  A call whose longest sequence has more may hold short ones too: both kernels then, each
-    // leaving the other's sequences out.
-    const int FEW = 2 * static_cast<int64_t>(c->num_seqs) * c->Hkv <= flat::device_sm_count() ? 16 : 64;
+    // Rows of a sequence and key head (new tokens times heads a group): up to FEW the warp-level products, whose tiles have sixteen
+    // rows, beyond the tcgen05 form, whose tiles have 128 and which reads the cache once for all of them (us, the one / the other: 12
+    // sequences of 4-32K tokens, 4 key heads, 28 rows 100 / 131, 64 rows 181 / 133; 2 of 1-2K, 8 key heads, 40 rows 16 / 31).  A call
+    // whose longest sequence has more may hold short ones too: both kernels then, each leaving the other's sequences out.
+    constexpr int FEW = 64;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool many = static_cast<int64_t>(p->max_new) * (p->Hq / c->Hkv) > FEW, few = !many || c->num_seqs > 1;
     int launches = 0;

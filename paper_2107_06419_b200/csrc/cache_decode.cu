@@ -33,13 +33,15 @@ namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int HALF_BYTES = 4096, CHUNK_BYTES = 2 * HALF_BYTES;            // a chunk's keys, then its values
-// RG: row groups of eight in a tile.  One: three CTAs an SM and two chunks a warp in the ring; two need the registers of two CTAs.
-// (Four, with the queries in shared memory: 48 items of 28 rows 98 us, in two tiles of sixteen 100; its 1,100 instructions a chunk are
-// too long a chain for eight warps an SM.)
+// RG: row groups of eight in a tile.  Three CTAs an SM and two chunks a warp in the ring; with two row groups that takes the queries
+// out of the registers into memory that the team shares, and a team of one warp, which would need its own, has two CTAs and three chunks.
+// (Four row groups: 48 items of 28 rows 98 us, in two tiles of sixteen 100; 1,100 instructions a chunk are too long a chain for
+// eight warps an SM.)
 constexpr int TILE = 16;
-__host__ __device__ constexpr int CTAS(int RG) { return RG == 1 ? 3 : 2; }
-__host__ __device__ constexpr int STAGES(int RG) { return RG == 1 ? 2 : 3; }
-__host__ __device__ constexpr int SMEM_BYTES(int RG) { return WARPS * STAGES(RG) * CHUNK_BYTES; }
+__host__ __device__ constexpr bool SHARED_Q(int RG, int TEAM) { return RG == 2 && TEAM > 1; }
+__host__ __device__ constexpr int CTAS(int RG, int TEAM) { return RG == 1 || SHARED_Q(RG, TEAM) ? 3 : 2; }
+__host__ __device__ constexpr int STAGES(int RG, int TEAM) { return CTAS(RG, TEAM) == 3 ? 2 : 3; }
+__host__ __device__ constexpr int SMEM_BYTES(int D, int RG, int TEAM) { return WARPS * STAGES(RG, TEAM) * CHUNK_BYTES + (SHARED_Q(RG, TEAM) ? RG * D * 16 : 0); }
 constexpr int ALIGN_COST = 5;                                             // chunks
 // Aligned parts have at least this many chunks, one a warp; of a long item more: its parts are joined one after the other, sixteen in
 // flight (0.03 us each), a warp's chunk takes 0.6 us, so P parts of n chunks take about n / (4 P) 0.6 + 0.03 P us, least at P = sqrt(5 n).
@@ -115,12 +117,13 @@ __device__ __forceinline__ float two_to(int e) {         // 2^e for any e: 0 bel
 // TEAM: warps of a team (4 or 1).  RG: row groups of eight in a tile (1: no sequence has more than eight rows).  SMALL: pages of less
 // than a chunk.
 template <int D, int RG, int TEAM, bool SMALL>
-__global__ void __launch_bounds__(THREADS, CTAS(RG))
+__global__ void __launch_bounds__(THREADS, CTAS(RG, TEAM))
 cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     constexpr int CH = HALF_BYTES / D;                   // tokens of a chunk: 32 (d = 128) or 64
     constexpr int PIECES = D / 16, RPI = 32 / PIECES;    // 16-byte pieces of a row; rows that a copy instruction brings
     constexpr int NT = CH / 16;                          // logit blocks of sixteen keys
-    constexpr int STAGES = flat::STAGES(RG);
+    constexpr int STAGES = flat::STAGES(RG, TEAM);
+    constexpr bool SHARED_Q = flat::SHARED_Q(RG, TEAM);
     constexpr int JOIN = D + 4;                          // floats from row to row where the warps join: eight lanes' rows in eight banks' distance
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ float warp_lse[WARPS][TILE];
@@ -311,7 +314,8 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 
         // ------------------------------------------------------------ queries: half precision, a power of two taken out of each row
         // Slice 4 x + w of the contraction: a lane's features 16 (t + 4 x) + 4 w .. + 3, the ones that it reads of a key
-        uint32_t qb[D / 16][RG][2];
+        uint32_t qb[SHARED_Q ? 1 : D / 16][RG][2];
+        const uint32_t queries = ptx::smem_u32(smem) + WARPS * STAGES * CHUNK_BYTES + lane * 8;      // (SHARED_Q) [slice][row group][lane]
         float unit[RG][2];                               // of the rows 8 r + 2 t, + 1: logits' scale, keys that they see
         int nrow[RG][2];
 #pragma unroll
@@ -350,10 +354,17 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                 for (int w = 0; w < 4; ++w) {
                     const uint4& v = raw[x][w >> 1];
                     const uint32_t lo = w & 1 ? v.z : v.x, hi = w & 1 ? v.w : v.y;
-                    qb[4 * x + w][r][0] = pack_half2(__uint_as_float(lo << 16) * up, __uint_as_float(lo & 0xffff0000u) * up);
-                    qb[4 * x + w][r][1] = pack_half2(__uint_as_float(hi << 16) * up, __uint_as_float(hi & 0xffff0000u) * up);
+                    const uint32_t q0 = pack_half2(__uint_as_float(lo << 16) * up, __uint_as_float(lo & 0xffff0000u) * up);
+                    const uint32_t q1 = pack_half2(__uint_as_float(hi << 16) * up, __uint_as_float(hi & 0xffff0000u) * up);
+                    if (!SHARED_Q) {
+                        qb[SHARED_Q ? 0 : 4 * x + w][r][0] = q0;
+                        qb[SHARED_Q ? 0 : 4 * x + w][r][1] = q1;
+                    } else if (warp == w) {              // (every warp has them, each leaves a quarter)
+                        asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(queries + ((4 * x + w) * RG + r) * 256), "r"(q0), "r"(q1) : "memory");
+                    }
                 }
         }
+        if (SHARED_Q) __syncthreads();
         int tok0, gh0;
         place_of(0, tok0, gh0);
         const long long lim0 = static_cast<long long>(tok0) + 1 + sp.len - sp.n;     // keys that every row sees
@@ -411,25 +422,55 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             // logits, keys as rows: c[i][r]: keys 16 i + krow (0, 1) and 16 i + krow + 2 (2, 3) of the rows 8 r + 2 t and 8 r + 2 t + 1
             float c[NT][RG][4];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int r = 0; r < RG; ++r)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) c[i][r][e] = 0.f;
-                const uint32_t row = ks + (i * 16 + krow) * D;
+            if (SHARED_Q) {                              // slice by slice: its queries serve all blocks
 #pragma unroll
                 for (int x = 0; x < D / 64; ++x) {
-                    uint32_t w[4], v[4];
+                    uint32_t w[NT][4], v[NT][4];
                     const int at = (D == 128 ? (t + 4 * x) ^ ((krow & 1) << 2) : t) * 16;
-                    lds16(row + at, w);
-                    lds16(row + 2 * D + at, v);
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        lds16(ks + (i * 16 + krow) * D + at, w[i]);
+                        lds16(ks + (i * 16 + krow + 2) * D + at, v[i]);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        uint32_t a[4];
-                        halves(w[e], a[0], a[2]);
-                        halves(v[e], a[1], a[3]);
+                        uint32_t q[RG][2];
 #pragma unroll
-                        for (int r = 0; r < RG; ++r) mma16(c[i][r], a, qb[4 * x + e][r][0], qb[4 * x + e][r][1]);
+                        for (int r = 0; r < RG; ++r)
+                            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(q[r][0]), "=r"(q[r][1]) : "r"(queries + ((4 * x + e) * RG + r) * 256));
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) {
+                            uint32_t a[4];
+                            halves(w[i][e], a[0], a[2]);
+                            halves(v[i][e], a[1], a[3]);
+#pragma unroll
+                            for (int r = 0; r < RG; ++r) mma16(c[i][r], a, q[r][0], q[r][1]);
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const uint32_t row = ks + (i * 16 + krow) * D;
+#pragma unroll
+                    for (int x = 0; x < D / 64; ++x) {
+                        uint32_t w[4], v[4];
+                        const int at = (D == 128 ? (t + 4 * x) ^ ((krow & 1) << 2) : t) * 16;
+                        lds16(row + at, w);
+                        lds16(row + 2 * D + at, v);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t a[4];
+                            halves(w[e], a[0], a[2]);
+                            halves(v[e], a[1], a[3]);
+#pragma unroll
+                            for (int r = 0; r < RG; ++r) mma16(c[i][r], a, qb[SHARED_Q ? 0 : 4 * x + e][r][0], qb[SHARED_Q ? 0 : 4 * x + e][r][1]);
+                        }
                     }
                 }
             }
@@ -687,11 +728,11 @@ size_t counter_bytes() { return (most_teams() * sizeof(int) + 255) & ~size_t(255
 
 template <int D, int RG, int TEAM, bool SMALL>
 int launch(const DecodeArgs& p, cudaStream_t st) {
-    if (!ensure_dynamic_smem<cache_decode_kernel<D, RG, TEAM, SMALL>>(SMEM_BYTES(RG))) return FLAT_ERR_CUDA;
+    if (!ensure_dynamic_smem<cache_decode_kernel<D, RG, TEAM, SMALL>>(SMEM_BYTES(D, RG, TEAM))) return FLAT_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(device_sm_count() * CTAS(RG));
+    cfg.gridDim = dim3(device_sm_count() * CTAS(RG, TEAM));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = SMEM_BYTES(RG);
+    cfg.dynamicSmemBytes = SMEM_BYTES(D, RG, TEAM);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

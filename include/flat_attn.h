@@ -271,7 +271,7 @@ int flat_attn_varlen_fwd(const void* Q, const void* K, const void* V, void* O,
  * same strides; otherwise what is written may overlap nothing else, itself included (an output stride of 0 along more than one
  * element is FLAT_ERR_SHAPE).  positions: device, position of token n of batch b at b * positions_stride_b + n (a stride of 0 shares
  * them), any 32-bit value; NULL: token n has position n.  bf16 or fp32; cosines, sines and products in fp32, rounded once.
- * d in {16, 32, 64, 128}, rotary_dim even, 2 <= rotary_dim <= d (FLAT_ERR_UNSUPPORTED).  B <= 65535, B * N <= 2^31 - 1, (Hq + Hk) <= 65535.
+ * d in {16, 32, 64, 128}, rotary_dim even, 2 <= rotary_dim <= d (FLAT_ERR_UNSUPPORTED).  B <= 65535, B * N <= 2^31 - 256, Hq + Hk <= 65535.
  * One kernel; pointers 16-byte aligned (positions 4, table 8).  `p` is a HOST pointer, read before the call returns.
  */
 enum { FLAT_ROPE_PLAIN = 0, FLAT_ROPE_LINEAR = 1, FLAT_ROPE_BASE = 2, FLAT_ROPE_PARTS = 3 };
@@ -318,9 +318,12 @@ int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream);
  * flat_attn_cache_fwd: Q, O [total, Hq, d] bf16 (strides as above), Hq = G * Hkv: query head h reads key head h / G, G <= 128.  causal = 1:
  * query i of n sees the keys j <= i + length - n; 0: all of its sequence.  O = 0 (and lse = -inf) for a row whose keys are all left out.
  * Cache entries of a sequence must be finite; what lies behind its length in its last page is ignored, NaN included.
- * lse: optional [total, Hq] fp32, as in flat_attn_params_t.  Keys and values are used unrounded (e4m3 is exact in the half
- * precision of the products), Q as half-precision numbers scaled by a power of two for each row (unrounded where a feature is within 2^-28 of
- * the row's largest), weights rounded to half precision, sums in fp32.  The keys of long sequences are split over CTAs and joined in a fixed order: same bits every time.
+ * lse: optional [total, Hq] fp32, as in flat_attn_params_t.  e4m3 is exact in the half precision of the products.  Queries enter them scaled
+ * by a power of two for each row (unrounded where a feature is within 2^-28 of the row's largest); where a sequence has more than 64
+ * rows (new tokens times G) keys and values enter scaled relative to the largest page of the sequence and head (unrounded in pages
+ * whose scale is within 2^-21 of it); weights are rounded to half precision at 2^9 to 2^15 times their size; sums are fp32.  The keys of long
+ * sequences are split over CTAs and joined in a fixed order: same bits every time.  One kernel, or two in a call that may hold sequences
+ * of more than 64 rows and others.
  * workspace: device, at least flat_attn_cache_workspace_bytes(Hq, Hkv, d) bytes on the device of the call, 256-byte aligned, zeroed once by the caller; every call
  * leaves it ready for the next.  Calls that may run at the same time (other streams, captured graphs that overlap) need one each.
  */

@@ -102,7 +102,7 @@ bool apart(const long long* stride, const long long* size, int n, long long row)
 int validate_rope(const flat_attn_rope_params_t* p) {
     if (!p || !p->Q || !p->Qr || !p->table || !p->K != !p->Kr) return FLAT_ERR_NULL;
     if (p->B < 1 || p->N < 1 || p->Hq < 1 || (p->K && p->Hk < 1) || !isfinite(p->amplitude)) return FLAT_ERR_SHAPE;
-    if (p->B > 65535 || static_cast<int64_t>(p->B) * p->N > 0x7fffffff || static_cast<int64_t>(p->Hq) + (p->K ? p->Hk : 0) > 65535) return FLAT_ERR_SHAPE;
+    if (p->B > 65535 || static_cast<int64_t>(p->B) * p->N > 0x7fffff00 || static_cast<int64_t>(p->Hq) + (p->K ? p->Hk : 0) > 65535) return FLAT_ERR_SHAPE;
     if (p->dtype != FLAT_DTYPE_BF16 && p->dtype != FLAT_DTYPE_F32) return FLAT_ERR_UNSUPPORTED;
     if (p->d != 16 && p->d != 32 && p->d != 64 && p->d != 128) return FLAT_ERR_UNSUPPORTED;
     if (p->rotary_dim < 2 || p->rotary_dim > p->d || p->rotary_dim % 2 != 0) return FLAT_ERR_UNSUPPORTED;

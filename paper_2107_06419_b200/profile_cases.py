@@ -7,7 +7,9 @@ CASE: fused | fused_lse | naive | backward | fp32 | bias | layernorm | layer.  T
 device); inputs are the seeded generator's.  Prints the mean launch time from CUDA events.  `fp32` runs the
 split-tf32 tensor-core kernel (`--variant 1`: the FFMA kernel).
 Cases with sizes of their own, on random inputs: decode (B16 H16 1 x 8192, d 128, 25-100 % of the cache filled) | small (B64 H8
-1000^2, d 32) | packed (32 sequences of 40 to 2000 tokens, 12 heads, d 64) | fp32_d128 (B2 H16 4096^2) | fc (512 x 3072 -> 768).
+1000^2, d 32) | packed (32 sequences of 40 to 2000 tokens, 12 heads, d 64) | fp32_d128 (B2 H16 4096^2) | fc (512 x 3072 -> 768) |
+rope (B8 H16 2048, d 128) | append (6 prompts of 2000 tokens, 8 key heads, d 128, pages of 16) | cache (64 sequences of 1000 to 16384 tokens in the 8-bit
+paged cache, one query each, 32 heads on 8, d 128) | cache_prompt (4096 queries behind 28672 cached tokens, 8 heads on 2, d 128).
 """
 from __future__ import annotations
 
@@ -50,9 +52,40 @@ def _fc():
     return (lambda: api.flat_fc_fwd(X, W, Y, status=status)), 2.0 * 512 * 3072 * 768, status
 
 
+def _rope():
+    torch.manual_seed(1)
+    Q, K = _normal(8, 16, 2048, 128), _normal(8, 16, 2048, 128)
+    Qr, Kr, status = torch.empty_like(Q), torch.empty_like(K), torch.zeros(1, dtype=torch.int32, device="cuda")
+    table, amplitude = api.flat_attn_rope_table(128)
+    return (lambda: api.flat_attn_rope_fwd(Q, K, table, Qr, Kr, amplitude=amplitude)), 0.0, status
+
+
+def _cache(lens, new, Hq, Hkv, d, page, append=False):
+    torch.manual_seed(1)
+    counts = [-(-m // page) for m in lens]
+    order = torch.randperm(sum(counts), device="cuda").to(torch.int32)
+    table = torch.zeros(len(lens), max(counts), dtype=torch.int32, device="cuda")
+    for s, c in enumerate(counts):
+        table[s, :c] = order[sum(counts[:s]):sum(counts[:s]) + c]
+    k, v = ((_normal(sum(counts), Hkv, page, d) * 80).clamp(-448, 448).to(torch.float8_e4m3fn) for _ in range(2))
+    ke, ve = (torch.randint(118, 123, (sum(counts), Hkv), device="cuda").to(torch.uint8) for _ in range(2))
+    cu = torch.tensor([0] + new, dtype=torch.int32).cumsum(0).to(torch.int32).cuda()
+    sl, status = torch.tensor(lens, dtype=torch.int32).cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    if append:
+        K, V = _normal(sum(new), Hkv, d), _normal(sum(new), Hkv, d)
+        return (lambda: api.flat_attn_cache_append(K, V, k, v, ke, ve, table, cu, sl, max(new), status=status)), 0.0, status
+    Q = _normal(sum(new), Hq, d)
+    O, work = torch.empty_like(Q), torch.zeros(api.flat_attn_cache_workspace_bytes(Hq, Hkv, d), dtype=torch.uint8, device="cuda")
+    step = lambda: api.flat_attn_cache_fwd(Q, O, k, v, ke, ve, table, cu, sl, max(new), d ** -0.5, work, causal=True, status=status)
+    return step, 4.0 * Hq * d * sum(n * m - n * (n - 1) // 2 for n, m in zip(new, lens)), status
+
+
 # case -> (step, floating-point operations, status word), with sizes of its own
 OWN = {"decode": lambda: _attention(16, 16, 1, 8192, 128, filled=0.25), "small": lambda: _attention(64, 8, 1000, 1000, 32),
-       "fp32_d128": lambda: _attention(2, 16, 4096, 4096, 128, torch.float32), "packed": _packed, "fc": _fc}
+       "fp32_d128": lambda: _attention(2, 16, 4096, 4096, 128, torch.float32), "packed": _packed, "fc": _fc,
+       "rope": _rope, "append": lambda: _cache([2500] * 6, [2000] * 6, 8, 8, 128, 16, append=True),
+       "cache": lambda: _cache([1000 + 244 * i for i in range(64)], [1] * 64, 32, 8, 128, 64),
+       "cache_prompt": lambda: _cache([32768], [4096], 8, 2, 128, 128)}
 
 
 def main():

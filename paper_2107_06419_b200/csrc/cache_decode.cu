@@ -8,12 +8,21 @@
 //
 // What bounds it: device memory, 2 d bytes a token and key head against 4 d FLOP a query row.  The rows of a unit are the queries
 // of one sequence times the G query heads that share a key head, sixteen to a tile, so the cache is read once for up to sixteen rows.
+// Keys (and, in the second product, features) are the rows of the products and queries their columns, so that eight rows are one
+// column block; ldmatrix transposes the values' bytes.  64 sequences of 8,192 tokens, 32 query heads on 8, d = 128 (1.07 GB): 164 us,
+// 6.56 TB/s, the rate of a copy; of 1,000 to 16,384 tokens (852 MB) 141 us, 6.05 TB/s, with queries as rows (twice the products for eight
+// rows) 176, with conversions through the header's structures (two more instructions for two values) 215.  What is left where an
+// item is short is the chain of a part -- table entry, tokens, products, join, about 3 us -- and 2 us of deal: one sequence of 2,000 tokens
+// 8.8 us, 16 sequences of 2-8K with 16 heads of 64 in pages of sixteen 31.8 (4.0 TB/s).  With two row groups twelve warps an SM do not cover
+// the chain of a chunk (750 instructions): 12 sequences of 4-32K, 4 key heads, 28 rows in two tiles 91 us (2.5 TB/s of the cache read
+// once).
+//
 // Work is dealt by chunks of 8 KB (keys and values of 32 tokens, d = 128): all chunks of all (sequence, key head, row tile) in one
-// row, an equal share of neighbouring chunks to each team.  A team is a CTA (four warps, which take a part's chunks in turn
-// and join through shared memory), or one warp where there are more items than warps.  An item that ends up in several teams
-// is joined by whichever of them comes last, from their normalised outputs and log-sums, in the order of the keys.
-// Every warp keeps its own ring of three chunks (cp.async, 16 bytes a lane and instruction: any page size and order, tokens behind the
-// length filled with zeros), so no barrier is in the loop.
+// row, an equal share of neighbouring chunks to each team, or, where there are few items, a part of one item each.  A team is a
+// CTA (four warps, which take a part's chunks in turn and join through shared memory), or one warp where there are more items than
+// warps.  An item that ends up in several teams is joined by whichever of them comes last, from their normalised outputs and
+// log-sums, in the order of the keys.  Every warp keeps its own ring of chunks (cp.async, 16 bytes a lane and instruction: any page size and order, tokens
+// behind the length filled with zeros), so no barrier is in the loop.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>

@@ -2,18 +2,26 @@
 //
 // The rows of a sequence and key head are its queries times the G query heads of the group; an item is a slab of 256 of them, two tiles
 // of 128, against the keys that they see, in steps of 64.  Logits and outputs are tcgen05 products in half precision with fp32
-// accumulators in TMEM.  e4m3 numbers are exact in half precision; four warps bring the pages (cp.async into memory of their own,
-// no barrier), turn them into half-precision tiles in the 128-byte swizzle and take the page's scale into them, relative to the largest
-// of the sequence and head: k 2^(ek - EK + 6), exact until 2^-30 of the largest value becomes subnormal.  So the softmax sees one
-// scale.  Queries are scaled by a power of two a row into half precision (it goes into the row's softmax constant); weights are 2^9 w,
-// rounded to half precision.
+// accumulators in TMEM.  e4m3 numbers are exact in half precision: one warp looks the pages up and copies them (bulk copies of sixteen
+// tokens), four warps turn them into half-precision tiles in the 128-byte swizzle and take the page's scale into them, relative to the
+// largest of the part's pages: k 2^(ek - EK + 6), exact in pages whose scale is within 2^-21 of it.  So the softmax sees one scale.
+// Queries are scaled by a power of two a row into half precision (it goes into the row's softmax constant); weights are 2^9 w, rounded
+// to half precision.
 //
 // CTA = 512 threads: warps 0-3 / 4-7 softmax of tile A / B (thread = row = TMEM lane), warps 8 / 9 MMA issuers of tile A / B (one
-// elected lane), warps 10, 11 idle (they complete a warpgroup for the register hand-over), warps 12-15 bring and convert keys and values.
+// elected lane), warp 10 look-ups and copies, warp 11 idle (it completes a warpgroup for the register hand-over), warps 12-15 convert.
 // TMEM columns: S(t, b) 128 t + 64 b (b = step parity), P over the first 32 of them, O_t 256 + 128 t.
 // The softmax takes no row maximum after the first step: any reference gives the exact softmax; a step whose row sum passes 60,000
-// (a weight could pass the largest half-precision number) is redone with a fresh maximum.  One exponential in four goes through a
+// (a weight could pass the largest half-precision number) is redone with a fresh maximum.  One exponential in eight goes through a
 // polynomial on the FMA pipe.  Every wait is bounded (tc_common.cuh); on expiry the CTA aborts cleanly and reports a code.
+//
+// What bounds it, d = 128: shared memory's port and the softmax warps together.  A step of both tiles moves 1,024 cycles of operands
+// for the tensor pipe (A of the logits alone 512) and 512 of conversions; its exponentials take 1,010 cycles of the exponent unit;
+// measured 1,920 cycles (softmax 1,270 of work and 330 of waiting for logits).  4,096 queries behind 28,672 tokens, 32 heads on 8:
+// 1,720 us in the first 20 ms of launches (1,200 TFLOP/s), 1,960 at the power cap (1,050; a cuBLAS GEMM 1,639 and 1,396).  d = 64: the exponentials,
+// 550 TFLOP/s.  Tried: the converters' own cp.async (their addresses were half of a step: 587 us against 522 on 128 items), logits
+// of two steps in one product (N = 128, one buffer a tile: 567; d = 64 494 against 466), no polynomial 534 and one in four 521.
+// Items: those of the last round, or all if they are fewer than the SMs, are split along the keys (2 x 4 x 512 rows over 32,768 keys 537 -> 108 us).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -10,7 +10,11 @@
 // rad), and after taking off the nearest quarter turn what is left has 29 bits, rounded to fp32: 2.4e-8 rad.
 //
 // Bound: device memory, every feature read once and written once.  A CTA takes a few tokens and all their heads, computes the
-// tokens' cosines and sines once (shared memory) and rotates with 16-byte loads and stores, four pairs of them in flight a thread.
+// tokens' cosines and sines once (shared memory); a thread keeps its token and its place in the row, so those it needs stay in
+// registers while it goes from head to head with 16-byte loads and stores.  Measured: 8 x 16 heads of 128 x 2,048 tokens, queries and keys
+// (269 MB) 44 us, 6.1 TB/s, 0.93 of a copy; 4 x 16 heads of 64 x 4,096, half of each in neighbouring pairs (134 MB) 23.6 us (51
+// with the angles read from shared memory for every vector).  An odd number of pairs, or one that no vector divides, in the half layout: partners one by
+// one, 43 us where 22 would be the rate of the others.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>

@@ -154,6 +154,19 @@ def test_relative_positions(api):
     assert float((dots - dots[0]).abs().max()) <= 4 * bound
 
 
+def test_more_than_2_31_elements(api):
+    N, H, d = 70000, 256, 128
+    x = torch.empty(1, H, N, d, dtype=torch.bfloat16, device="cuda").uniform_(-1, 1)
+    table, a = api.flat_attn_rope_table(d)
+    f, _ = frequencies(d)
+    y = torch.empty_like(x)
+    api.flat_attn_rope_fwd(x, None, table, y, None)
+    torch.cuda.synchronize()
+    at = torch.tensor([0, 5, 33333, N - 1], device="cuda")
+    for h in (0, 100, H - 1):
+        check(y[0, h, at], x[0, h, at], f, a, at, False)
+
+
 def test_other_stream_and_graph(api):
     table, _ = api.flat_attn_rope_table(128)
     Q, K = torch.randn(2, 4, 300, 128, device="cuda").to(torch.bfloat16), torch.randn(2, 2, 300, 128, device="cuda").to(torch.bfloat16)

@@ -21,7 +21,8 @@
 // 1,720 us in the first 20 ms of launches (1,200 TFLOP/s), 1,960 at the power cap (1,050; a cuBLAS GEMM 1,639 and 1,396).  d = 64: the exponentials,
 // 550 TFLOP/s.  Tried: the converters' own cp.async (their addresses were half of a step: 587 us against 522 on 128 items), logits
 // of two steps in one product (N = 128, one buffer a tile: 567; d = 64 494 against 466), no polynomial 534 and one in four 521.
-// Items: those of the last round, or all if they are fewer than the SMs, are split along the keys (2 x 4 x 512 rows over 32,768 keys 537 -> 108 us).
+// Items: those of the last round, or all if they are fewer than the SMs, are split along the keys (128 queries, 32 heads on 8, over
+// 32,768 keys: 537 -> 108 us).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -79,32 +79,33 @@ __device__ __forceinline__ float two_to(int e) {         // 2^e for any e: 0 bel
     return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
 }
 
-// p_i = 2^(s_i * unit + neg_m) of 64 logits, rounded to half precision into 32 TMEM columns at `p_addr`; returns the fp32 sum of the
+// p_i = 2^(s_i * unit + neg_m) of 64 logits, rounded to half precision into 32 TMEM columns at `p_addr`, sixteen logits at a time (128 items
+// of d = 128 518 us against 530 by the 32, d = 64 453 against 465); returns the fp32 sum of the
 // unrounded p.  TAIL: only the first `nvalid` take part, and of those not the groups of sixteen in `out`.
 template <bool TAIL>
 __device__ __forceinline__ float exp_store(const uint32_t (&s)[BN], float unit, float neg_m, uint32_t p_addr, int nvalid, int out) {
     uint64_t sum0 = 0ull, sum1 = 0ull;
     const uint64_t unit2 = pack2(unit, unit), neg_m2 = pack2(neg_m, neg_m);
 #pragma unroll
-    for (int c = 0; c < BN / 32; ++c) {
-        uint32_t pk[16];
-        float p[32];
+    for (int c = 0; c < BN / 16; ++c) {
+        uint32_t pk[8];
+        float p[16];
 #pragma unroll
-        for (int i = 0; i < 32; i += 2)
-            unpack2(fma2(pack2(__uint_as_float(s[c * 32 + i]), __uint_as_float(s[c * 32 + i + 1])), unit2, neg_m2), p[i], p[i + 1]);
+        for (int i = 0; i < 16; i += 2)
+            unpack2(fma2(pack2(__uint_as_float(s[c * 16 + i]), __uint_as_float(s[c * 16 + i + 1])), unit2, neg_m2), p[i], p[i + 1]);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < 16; ++i) {
             p[i] = !TAIL && (i & 7) == POLY_LANE ? ex2_poly(p[i]) : ex2_approx(p[i]);
-            if (TAIL && (c * 32 + i >= nvalid || (out >> (2 * c + i / 16) & 1))) p[i] = 0.f;
+            if (TAIL && (c * 16 + i >= nvalid || (out >> ((c * 16 + i) / 16) & 1))) p[i] = 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
+        for (int i = 0; i < 16; i += 4) {
             sum0 = add2(sum0, pack2(p[i], p[i + 1]));
             sum1 = add2(sum1, pack2(p[i + 2], p[i + 3]));
             pk[i / 2] = pack_half2(p[i], p[i + 1]);
             pk[i / 2 + 1] = pack_half2(p[i + 2], p[i + 3]);
         }
-        tmem_st_x16(p_addr + c * 16, pk);
+        tmem_st_x8(p_addr + c * 8, pk);
     }
     float a, b, cc, d;
     unpack2(sum0, a, b);

@@ -544,6 +544,11 @@ def _rows_contiguous(name, t, dtype, shape):
         raise ValueError("%s must be a %s tensor of shape %s whose last dimension is contiguous" % (name, dtype, tuple(shape)))
 
 
+def _count(n):
+    """A number of tokens for the library, which refuses those out of range (ctypes would cut them to 32 bits)."""
+    return min(max(int(n), -1), 2 ** 31 - 1)
+
+
 def _step(t, dim):
     return 0 if t.shape[dim] == 1 else t.stride(dim)
 
@@ -640,7 +645,7 @@ def flat_attn_cache_append(K, V, k_cache, v_cache, k_exp, v_exp, page_table, cu_
     _rows_contiguous("V", V, torch.bfloat16, shape)
     _here(K=K, V=V)
     _check(_lib.flat_attn_cache_append(ctypes.byref(c), _ptr(K), _ptr(V), K.shape[0], _step(K, 0), _step(K, 1), _step(V, 0), _step(V, 1),
-                                       int(max_new), _stream_ptr(stream)))
+                                       _count(max_new), _stream_ptr(stream)))
     return k_cache, v_cache
 
 
@@ -674,7 +679,7 @@ def flat_attn_cache_fwd(Q, O, k_cache, v_cache, k_exp, v_exp, page_table, cu_seq
     p = flat_attn_cache_fwd_params_t()
     p.Q, p.O, p.Hq, p.total = Q.data_ptr(), O.data_ptr(), Q.shape[1], Q.shape[0]
     p.q_stride_t, p.q_stride_h, p.o_stride_t, p.o_stride_h = _step(Q, 0), _step(Q, 1), _step(O, 0), _step(O, 1)
-    p.max_new, p.causal, p.scale = int(max_seqlen_q), 1 if causal else 0, float(scale)
+    p.max_new, p.causal, p.scale = _count(max_seqlen_q), 1 if causal else 0, float(scale)
     p.lse = None if lse is None else lse.data_ptr()
     p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
     _check(_lib.flat_attn_cache_fwd(ctypes.byref(c), ctypes.byref(p), _stream_ptr(stream)))

@@ -87,10 +87,10 @@ struct Args {
         return 0;
     }
     // The status word: an address on the GPU is all the library asks of it.
-    int32_t* status() {
+    int32_t* status(bool on_current = false) {
         PyObject* o = next();
         if (o == Py_None) return nullptr;
-        if (bad || !THPVariable_CheckExact(o) || !THPVariable_Unpack(o).is_cuda()) { bad = true; return nullptr; }
+        if (bad || !THPVariable_CheckExact(o) || !THPVariable_Unpack(o).is_cuda() || (on_current && !here(THPVariable_Unpack(o)))) { bad = true; return nullptr; }
         return static_cast<int32_t*>(THPVariable_Unpack(o).data_ptr());
     }
     // None (the current stream of the current device), an address, or an object with a cuda_stream.
@@ -388,7 +388,7 @@ PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor *K = a.strided(at::kBFloat16), *V = a.strided(at::kBFloat16);
     if (a.bad || !cache_args(a, c)) return no();
     const int most = a.whole();
-    c.status = a.status();
+    c.status = a.status(true);
     void* st = a.stream();
     a.end();
     if (a.bad || K->dim() != 3 || K->size(1) != c.Hkv || K->size(2) != c.d || !V->sizes().equals(K->sizes())) return no();
@@ -410,7 +410,7 @@ PyObject* cache_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor* work = a.local(at::kByte);
     p.causal = a.truth();
     const at::Tensor* lse = a.local(at::kFloat, true);
-    c.status = a.status();
+    c.status = a.status(true);
     void* st = a.stream();
     a.end();
     if (a.bad || Q->dim() != 3 || Q->size(2) != c.d || !small(Q->size(1)) || !O->sizes().equals(Q->sizes()) ||

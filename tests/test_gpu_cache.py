@@ -330,3 +330,17 @@ def test_append_bad_tables_and_captured(api):
     g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip((k, v, ke, ve), before))
+
+
+@pytest.mark.parametrize("most", [2 ** 32 + 1, 2 ** 31, 4, 0, -1, -2 ** 32 + 1])
+def test_counts_out_of_range(api, most):
+    """More new tokens a sequence than there are, or fewer than one, in 32 bits and beyond."""
+    gen = torch.Generator().manual_seed(12)
+    k, v, ke, ve, table = ref.make_cache(gen, [40], 2, 16, 64, "cuda")
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    args = (k, v, ke, ve, table, ints([0, 3]), ints([40]))
+    for call in (lambda: api.flat_attn_cache_append(x, x, *args, most),
+                 lambda: api.flat_attn_cache_fwd(x, torch.empty_like(x), *args, most, 0.1, workspace(api, 2, 2, 64))):
+        with pytest.raises(api.FlatAttnError) as e:
+            call()
+        assert e.value.code == 2

@@ -175,9 +175,10 @@ append_kernel(const __grid_constant__ AppendArgs p) {
     const int which = unit & 1, h = (unit >> 1) % heads, slot = (unit >> 1) / heads % slots, s = (unit >> 1) / heads / slots;
     Span sp{0, 0, 0};
     bool work = s < p.c.num_seqs && read_span(p.c, s, p.total, p.max_new, sp) && sp.n > 0;
+    // (tokens before the new ones and slots for them: up to 2^30 tokens each, so that the end of the last slot passes 31 bits)
     const int start = sp.len - sp.n, first_page = start / PAGE, index = first_page + slot;
     int page_id = 0;
-    work = work && index * PAGE < sp.len && read_page(p.c, s, index, page_id);
+    work = work && static_cast<unsigned>(index) * PAGE < static_cast<unsigned>(sp.len) && read_page(p.c, s, index, page_id);
     const int r0 = slot == 0 ? start - first_page * PAGE : 0;
     const int r1 = !work ? 0 : sp.len - index * PAGE < PAGE ? sp.len - index * PAGE : PAGE;
     const int row = tid / (D / 16), col = tid % (D / 16) * 16;

@@ -607,7 +607,9 @@ int flat_attn_cache_append(const flat_attn_cache_t* c, const void* K, const void
     if (!aligned16(K) || !aligned16(V)) return FLAT_ERR_ALIGN;
     flat_attn_cache_t q = *c;
     q.status = status_or_library_word(c->status);
-    const int r = flat::launch_cache_append(q, K, V, total, k_stride_t, k_stride_h, v_stride_t, v_stride_h, max_new, static_cast<cudaStream_t>(stream));
+    // (a sequence with more new tokens than it can be long is left out anyway: a grid for them would only be larger)
+    const int most = max_new < c->max_pages * c->page ? max_new : c->max_pages * c->page;
+    const int r = flat::launch_cache_append(q, K, V, total, k_stride_t, k_stride_h, v_stride_t, v_stride_h, most, static_cast<cudaStream_t>(stream));
     if (r == FLAT_OK) g_last_launches = 1;
     return r;
 }

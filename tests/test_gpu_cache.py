@@ -344,3 +344,50 @@ def test_counts_out_of_range(api, most):
         with pytest.raises(api.FlatAttnError) as e:
             call()
         assert e.value.code == 2
+
+
+@pytest.mark.parametrize("page", [16, 128])
+def test_append_at_the_greatest_length(api, page):
+    """A sequence of 2^30 tokens and room for as many new ones as a call may have (one token's memory, seen many times)."""
+    d, longest, n = 64, 1 << 30, 5
+    pages, total = longest // page, 2 ** 31 - 1
+    gen = torch.Generator().manual_seed(13)
+    k, v, ke, ve, _ = ref.make_cache(gen, [2 * page], 1, page, d, "cuda", spare=0)
+    table = torch.zeros(1, pages, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    x = torch.randn(1, 1, d, generator=gen).to(torch.bfloat16).cuda()
+    many = x.expand(total, 1, d)
+    want = [t.clone() for t in (k, v, ke, ve)]
+    for i in range(2):                                   # (what the page holds at its end, as a sequence of one page)
+        ref.append(x.double().expand(n, 1, d), want[i], want[2 + i], [[1]], [0, n], [page])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.flat_attn_cache_append(many, many, k, v, ke, ve, table, ints([0, n]), ints([longest]), total, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    for got, w in zip((k, v, ke, ve), want):
+        assert torch.equal(got.view(torch.uint8), w.view(torch.uint8))
+
+
+@pytest.mark.parametrize("new,longest,least_parts", [(1, 1 << 30, 400), (70, 1 << 26, 16)])
+def test_attention_over_one_page_many_times(api, new, longest, least_parts):
+    """A very long sequence whose table names one page again and again: the output is that page's, the log-sum its own and log(times)."""
+    d, page, sms = 64, 16, torch.cuda.get_device_properties(0).multi_processor_count
+    gen = torch.Generator().manual_seed(14)
+    k, v, ke, ve, _ = ref.make_cache(gen, [page], 1, page, d, "cuda", spare=0, exps=(114, 116))
+    table = torch.zeros(1, longest // page, dtype=torch.int32, device="cuda")
+    Q = torch.randn(new, 1, d, generator=gen).to(torch.bfloat16).cuda()
+    O, lse = torch.empty_like(Q), torch.empty(new, 1, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.flat_attn_cache_fwd(Q, O, k, v, ke, ve, table, ints([0, new]), ints([longest]), new, 0.125, workspace(api, 1, 1, d), causal=False, lse=lse, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    R, L, A, B = ref.attention(Q, k, v, ke, ve, [[0]], [0, new], [page], 0.125, False)
+    # Beside what check_attention counts, the roundings of long sums in fp32: a warp of a part adds up n weights a lane, half a step
+    # (2^-24 of the sum) each, and its outputs sixteen keys at a time, where the product may cut off a whole step (2^-23).  Parts of at least
+    # 1 / least_parts of the sequence; one token: four warps a part, an eighth of a warp's keys a lane; 70: a thread a row, 64 keys at a time.
+    least_parts = min(least_parts, 2 * sms)
+    keys = longest / least_parts / (4 if new == 1 else 1)
+    weights, outputs = keys / (8 if new == 1 else 64) * 2.0 ** -24, keys / 16 * 2.0 ** -23
+    logits = d * 2.0 ** -24 * B
+    assert ((lse.double() - (L + math.log(longest // page))).abs() <= logits + 2.0 ** -18 * (1 + 20) + weights).all()
+    assert ((O.double() - R).abs() <= 2.0 ** -8 * R.abs() + (2.0 ** -10 + 2 * logits[..., None] + weights + outputs) * A).all()

@@ -235,7 +235,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     unsigned steps_all = 0;                              // (used where there are fewer items than SMs: it fits then)
     for (int s = lane * per; s < s_end; ++s) {
         slabs = slabs_of(s, sp);
-        mine_all += slabs * cv.Hkv;
+        mine_all = min(mine_all + slabs * cv.Hkv, 0x3ffffff);          // (with offsets that go back and forth it could pass 31 bits)
         steps_all += static_cast<unsigned>(slabs * cv.Hkv) * ((sp.len + BN - 1) / BN);
     }
     // (up to 32 sequences: a lane keeps its one, and what the warp needs of any of them comes by shuffle)

@@ -508,14 +508,20 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             for (int i = 0; i < D / 8; ++i) v[i] = active && row < rows ? q[i] : make_uint4(0, 0, 0, 0);
             // the part's largest exponents of the keys and values, and whether a page is missing
             int ke = 0, ve = 0, bad = 0;
-            for (int i = (j0 * BN >> cv.page_shift) + threadIdx.x; i <= last_page; i += 256) {
-                int id;
-                if (read_page(cv, work.s, i, id)) {
-                    const int place = id * cv.Hkv + work.h;
-                    ke = max(ke, static_cast<int>(cv.k_exp[place]));
-                    ve = max(ve, static_cast<int>(cv.v_exp[place]));
-                } else {
-                    bad = 1;
+            for (int i = (j0 * BN >> cv.page_shift) + threadIdx.x; i <= last_page; i += 4 * 256) {
+                int place[4];                            // (four on their way: a place waits for its page)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    int id;
+                    place[u] = -1;
+                    if (i + 256 * u > last_page) continue;
+                    if (read_page(cv, work.s, i + 256 * u, id)) place[u] = id * cv.Hkv + work.h;
+                    else bad = 1;
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    ke = max(ke, place[u] >= 0 ? static_cast<int>(cv.k_exp[place[u]]) : 0);
+                    ve = max(ve, place[u] >= 0 ? static_cast<int>(cv.v_exp[place[u]]) : 0);
                 }
             }
             ke = __reduce_max_sync(0xffffffffu, ke);

@@ -79,38 +79,54 @@ __device__ __forceinline__ float two_to(int e) {         // 2^e for any e: 0 bel
     return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
 }
 
-// p_i = 2^(s_i * unit + neg_m) of 64 logits, rounded to half precision into 32 TMEM columns at `p_addr`, sixteen logits at a time (128 items
-// of d = 128 518 us against 530 by the 32, d = 64 453 against 465); returns the fp32 sum of the
-// unrounded p.  TAIL: only the first `nvalid` take part, and of those not the groups of sixteen in `out`.
+// Of sixteen logits p_i = 2^(s_i * unit + neg_m), rounded to half precision into eight TMEM columns at `p_addr`; the fp32 sums of the
+// unrounded p go to sum0 and sum1.  TAIL: only the first `nvalid` take part.
 template <bool TAIL>
-__device__ __forceinline__ float exp_store(const uint32_t (&s)[BN], float unit, float neg_m, uint32_t p_addr, int nvalid, int out) {
-    uint64_t sum0 = 0ull, sum1 = 0ull;
-    const uint64_t unit2 = pack2(unit, unit), neg_m2 = pack2(neg_m, neg_m);
+__device__ __forceinline__ void exp16(const uint32_t* s, uint64_t unit2, uint64_t neg_m2, uint32_t p_addr, int nvalid, uint64_t& sum0, uint64_t& sum1) {
+    uint32_t pk[8];
+    float p[16];
 #pragma unroll
-    for (int c = 0; c < BN / 16; ++c) {
-        uint32_t pk[8];
-        float p[16];
+    for (int i = 0; i < 16; i += 2) unpack2(fma2(pack2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), unit2, neg_m2), p[i], p[i + 1]);
 #pragma unroll
-        for (int i = 0; i < 16; i += 2)
-            unpack2(fma2(pack2(__uint_as_float(s[c * 16 + i]), __uint_as_float(s[c * 16 + i + 1])), unit2, neg_m2), p[i], p[i + 1]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            p[i] = !TAIL && (i & 7) == POLY_LANE ? ex2_poly(p[i]) : ex2_approx(p[i]);
-            if (TAIL && (c * 16 + i >= nvalid || (out >> ((c * 16 + i) / 16) & 1))) p[i] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            sum0 = add2(sum0, pack2(p[i], p[i + 1]));
-            sum1 = add2(sum1, pack2(p[i + 2], p[i + 3]));
-            pk[i / 2] = pack_half2(p[i], p[i + 1]);
-            pk[i / 2 + 1] = pack_half2(p[i + 2], p[i + 3]);
-        }
-        tmem_st_x8(p_addr + c * 8, pk);
+    for (int i = 0; i < 16; ++i) {
+        p[i] = !TAIL && (i & 7) == POLY_LANE ? ex2_poly(p[i]) : ex2_approx(p[i]);
+        if (TAIL && i >= nvalid) p[i] = 0.f;
     }
-    float a, b, cc, d;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        sum0 = add2(sum0, pack2(p[i], p[i + 1]));
+        sum1 = add2(sum1, pack2(p[i + 2], p[i + 3]));
+        pk[i / 2] = pack_half2(p[i], p[i + 1]);
+        pk[i / 2 + 1] = pack_half2(p[i + 2], p[i + 3]);
+    }
+    tmem_st_x8(p_addr, pk);
+}
+__device__ __forceinline__ float total(uint64_t sum0, uint64_t sum1) {
+    float a, b, c, d;
     unpack2(sum0, a, b);
-    unpack2(sum1, cc, d);
-    return (a + b) + (cc + d);
+    unpack2(sum1, c, d);
+    return (a + b) + (c + d);
+}
+// The weights of a step's 64 logits over the first half of their columns (sixteen at a time: 128 items of d = 128 518 us against 530 by
+// the 32, d = 64 453 against 465); returns their sum.
+__device__ __forceinline__ float exp_store(const uint32_t (&s)[BN], float unit, float neg_m, uint32_t s_addr) {
+    uint64_t sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+    for (int c = 0; c < BN / 16; ++c) exp16<false>(s + c * 16, pack2(unit, unit), pack2(neg_m, neg_m), s_addr + c * 8, 16, sum0, sum1);
+    return total(sum0, sum1);
+}
+// The same out of TMEM, for the first `nvalid` keys, of those not the groups of sixteen in `out` (a loop: this is rare, and the shorter the
+// kernel's code the better its common steps run).  A group's weights go over logits that have been read.
+__device__ __forceinline__ float exp_store_tail(float unit, float neg_m, uint32_t s_addr, int nvalid, int out) {
+    uint64_t sum0 = 0ull, sum1 = 0ull;
+#pragma unroll 1
+    for (int c = 0; c < BN / 16; ++c) {
+        uint32_t s[16];
+        tmem_ld_x16(s_addr + c * 16, s);
+        tc_wait_ld();
+        exp16<true>(s, pack2(unit, unit), pack2(neg_m, neg_m), s_addr + c * 8, out >> c & 1 ? 0 : nvalid - c * 16, sum0, sum1);
+    }
+    return total(sum0, sum1);
 }
 // The largest unit * s of the keys that take part.
 __device__ __forceinline__ float row_max(const uint32_t (&s)[BN], float unit, int nvalid, int out) {
@@ -144,6 +160,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+template <int N> struct Const { static constexpr int value = N; };
 struct PrefillArgs {
     CacheView c;
     const __nv_bfloat16* Q;
@@ -208,11 +225,22 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     __shared__ int scales[2 * GROUPS];                   // of sixteen tokens: the exponents of the keys and values, a byte each; -1: no page there
     const int warp = warp_index(), lane = threadIdx.x & 31;
     const CacheView& cv = p.c;
+    if (threadIdx.x == 32) {
+        for (int i = 0; i < LY::NUM_BARS; ++i)
+            mbar_init(&bars[i], i == LY::EXPS_READY ? 8
+                                : i < LY::K_EMPTY || (i >= LY::V_FULL && i < LY::V_EMPTY) || (i >= LY::P_FULL && i < LY::PV_DONE) || i >= LY::SCALE_EMPTY ? 4
+                                : (i >= LY::K_EMPTY && i < LY::V_FULL) || (i >= LY::V_EMPTY && i < LY::S_FULL) ? 2 : 1);
+        *abort_flag = 0;
+        top_exp[0] = top_exp[1] = any_bad = 0;
+        fence_mbar_init();
+    }
+    if (warp == 2) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
     // (the previous kernels of the stream have finished before the next one may start: a decode launch behind this one relies on it)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // ---------------------------------------------------------------- the CTA's work (every warp for itself)
+    // ---------------------------------------------------------------- the CTA's work, by one warp (by every warp for itself: 200 queries, 32 heads, 17.7 us against 17.3,
+    // 1,024 over 8,192 keys 143 against 139)
     // Items: sequence after sequence, their last slabs (under the causal mask the longest) first, the heads side by side.  Those of the last
     // round, fewer than there are SMs, are split along the keys into as many parts as find an SM.
     auto slabs_of = [&](int s, Span& sp) {
@@ -220,7 +248,8 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         const int rows = sp.n * p.G;
         return rows <= p.least_rows ? 0 : (rows + 2 * BM - 1) / (2 * BM);
     };
-    {
+    auto deal = [&] {
+    if (lane == 0) work.nsteps = 0;                      // (nothing to do)
     const int per = (cv.num_seqs + 31) / 32, s_end = min(lane * per + per, cv.num_seqs);
     auto before = [&](int v) {                           // of the lanes below and this one
 #pragma unroll
@@ -248,7 +277,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     };
     const int items = __reduce_add_sync(0xffffffffu, mine_all);
     if (items > p.most_items) {                          // (offsets that go back and forth: more rows than the tensors have)
-        if (cv.status && threadIdx.x == 0) atomicExch(cv.status, FLAT_CACHE_BAD_LENGTH);
+        if (cv.status && lane == 0) atomicExch(cv.status, FLAT_CACHE_BAD_LENGTH);
         return;
     }
     // All items in one round: parts of `each` steps, as many as there are SMs.  Several rounds: the last one's items in `split` parts each.
@@ -269,7 +298,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     }
     const int upto = before(mine_all), units = __shfl_sync(0xffffffffu, upto, 31);
     const int rest = each ? 0 : units % p.sms, whole = units - rest, split = rest ? min(p.sms / rest, 16) : 1, unit = blockIdx.x;
-    if (unit >= whole + rest * split) return;            // (the whole CTA)
+    if (unit >= whole + rest * split) return;
     const int entry = unit < whole ? unit : whole + (unit - whole) / split;      // among the units before the split
     const int from = __ffs(__ballot_sync(0xffffffffu, upto > entry)) - 1;
     int s = from * per, first = __shfl_sync(0xffffffffu, upto - mine_all, from);
@@ -290,7 +319,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     const int parts = each ? min(of, all_steps) : unit < whole ? 1 : most_parts(all_steps, split);
     const int part = each ? (entry - first) % of : unit < whole ? 0 : (unit - whole) % split;
     if (part >= parts) return;
-    if (threadIdx.x == 0) {
+    if (lane == 0) {
         const int j0 = all_steps * part / parts;
         work = Work{s, sp.q0, sp.len, sp.len - sp.n, h, rows, row0, n, j0, all_steps * (part + 1) / parts - j0, rows - row0 > BM};
         part_slot = parts == 1 ? -1 : each ? unit : unit - whole;
@@ -298,23 +327,18 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         part_count = parts;
         part_item = each ? unit - part : (unit - whole) / split;
     }
-    }
-    if (threadIdx.x == 32) {
-        for (int i = 0; i < LY::NUM_BARS; ++i)
-            mbar_init(&bars[i], i == LY::EXPS_READY ? 8
-                                : i < LY::K_EMPTY || (i >= LY::V_FULL && i < LY::V_EMPTY) || (i >= LY::P_FULL && i < LY::PV_DONE) || i >= LY::SCALE_EMPTY ? 4
-                                : (i >= LY::K_EMPTY && i < LY::V_FULL) || (i >= LY::V_EMPTY && i < LY::S_FULL) ? 2 : 1);
-        *abort_flag = 0;
-        top_exp[0] = top_exp[1] = any_bad = 0;
-        fence_mbar_init();
-    }
-    if (warp == 0) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
+    };
+    if (warp == 0) deal();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const uint32_t bars_s = smem_u32(bars), abort_s = smem_u32(const_cast<int*>(abort_flag)), base_s = smem_u32(base);
     const int nsteps = work.nsteps;
+    if (nsteps == 0) {                                   // (the whole CTA)
+        if (warp == 2) tmem_dealloc(tmem, 512);
+        return;
+    }
 
     if (warp >= 12) {
         // ------------------------------------------------------------ keys and values: e4m3 pages -> half-precision tiles
@@ -501,11 +525,31 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         const uint32_t my_bars = bars_s + 8 * (LY::S_FULL + 2 * t);       // S_FULL of the tile; P_FULL and PV_DONE 32 and 64 bytes on
         const int tok = (row < rows ? row : rows - 1) / p.G, head = work.h * p.G + (row < rows ? row - tok * p.G : 0), token = work.q0 + tok;
         float unit = 0.f;
+        // The warp's rows, RPI at a time, LPR lanes a row (queries in, outputs out; a lane a row asks for every sector twice: 200 queries, 32
+        // heads, 17.3 us against 14.6): f(i, row, token, head).
+        constexpr int LPR = D / 8, RPI = 32 / LPR;
+        const int piece = lane % LPR;
+        auto walk = [&](auto unrolled, auto f) {
+            int r = work.row0 + t * BM + (warp & 3) * 32 + lane / LPR, tk = r / p.G, g = r - tk * p.G;
+#pragma unroll (decltype(unrolled)::value)
+            for (int i = 0; i < D / 8; ++i) {
+                f(i, r, static_cast<int64_t>(work.q0) + tk, work.h * p.G + g);
+                r += RPI;
+                g += RPI;
+                while (g >= p.G) { g -= p.G; ++tk; }
+            }
+        };
+        // Of the walk's i-th row, the lane's piece: its place in the tile (128-byte swizzle).
+        auto spot = [&](int i) {
+            const int in = (warp & 3) * 32 + i * RPI + lane / LPR;
+            return base_s + t * Q_BYTES + (piece >> 3) * (BM * 128) + in * 128 + (((piece & 7) ^ (in & 7)) << 4);
+        };
         {
-            const uint4* q = reinterpret_cast<const uint4*>(p.Q + token * p.q_st + head * p.q_sh);
+            // (eight features a lane, LPR lanes a row: sectors of 32 bytes are asked for once)
             uint4 v[D / 8];
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) v[i] = active && row < rows ? q[i] : make_uint4(0, 0, 0, 0);
+            walk(Const<D / 8>{}, [&](int i, int r, int64_t tk, int hd) {
+                v[i] = r < rows ? *reinterpret_cast<const uint4*>(p.Q + tk * p.q_st + hd * p.q_sh + piece * 8) : make_uint4(0, 0, 0, 0);
+            });
             // the part's largest exponents of the keys and values, and whether a page is missing
             int ke = 0, ve = 0, bad = 0;
             for (int i = (j0 * BN >> cv.page_shift) + threadIdx.x; i <= last_page; i += 4 * 256) {
@@ -533,27 +577,27 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                 if (bad) any_bad = 1;
                 mbar_arrive(&bars[LY::EXPS_READY]);
             }
-            // the query row into half precision
-            float top = 0.f;
+            // the query rows into half precision, a power of two taken out of each
+            int my_e = 0;
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
                 const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                uint32_t m = w[0] & 0x7fff7fffu;         // magnitudes of two features: their bits are in their order
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u))));
-            }
-            int e = static_cast<int>(__float_as_uint(top) >> 23) - 127;  // the row's largest: 2^e to 2^(e + 1)
-            e = e < -100 ? -100 : e;
-            const float up = two_to(14 - e);
-            unit = p.scale_log2e * two_to(e - 14);
-            const uint32_t at = base_s + t * Q_BYTES + mine * 128;
+                for (int k = 1; k < 4; ++k) m = __vmaxu2(m, w[k] & 0x7fff7fffu);
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                for (int o = LPR / 2; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+                int e = static_cast<int>(max(m & 0xffffu, m >> 16) >> 7) - 127;     // the row's largest: 2^e to 2^(e + 1)
+                e = e < -100 ? -100 : e;
+                const int theirs = __shfl_sync(0xffffffffu, e, (lane % RPI) * LPR);
+                if (lane / RPI == i) my_e = theirs;
+                const float up = two_to(14 - e);
                 uint32_t x[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) x[k] = pack_half2(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xffff0000u) * up);
-                sts16(at + (i >> 3) * (BM * 128) + (((i & 7) ^ (mine & 7)) << 4), x[0], x[1], x[2], x[3]);
+                sts16(spot(i), x[0], x[1], x[2], x[3]);
             }
+            unit = p.scale_log2e * two_to(my_e - 14);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars[LY::Q_FULL + t]);
@@ -588,11 +632,13 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             bool careful = j == 0 || tail;
             float lt = 0.f;
             if (!careful) {
-                lt = exp_store<false>(x, unit, SHIFT - m_ref, s_addr, BN, 0);
+                lt = exp_store(x, unit, SHIFT - m_ref, s_addr);
                 careful = __any_sync(0xffffffffu, !(lt <= MOST_SUM));
-                if (careful) {           // (the weights went over the first half of the logits only)
+                if (careful) {           // (the weights went over the first half of the logits: they go back)
+                    tmem_st_x32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
                     tmem_ld_x32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
                     tc_wait_ld();
+                    tc_wait_st();
                 }
             }
             if (careful) {
@@ -617,7 +663,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                     }
                     m_ref = m_new;
                 }
-                lt = exp_store<true>(x, unit, m_ref == -INFINITY ? 0.f : SHIFT - m_ref, s_addr, nvalid, out);
+                lt = exp_store_tail(unit, m_ref == -INFINITY ? 0.f : SHIFT - m_ref, s_addr, nvalid, out);
             }
             l += lt;
             tc_wait_st();
@@ -633,7 +679,6 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             if (slot >= 0) p.part_lse[(slot * 2 + t) * BM + mine] = lse2;
             else if (p.lse && row < rows) p.lse[static_cast<int64_t>(token) * p.Hq + head] = lse2 * 0.6931471805599453f;
             tc_fence_after();
-            __nv_bfloat16* orow = p.O + token * p.o_st + head * p.o_sh;
             float4* prow = reinterpret_cast<float4*>(p.part_o) + (static_cast<int64_t>(slot) * (D / 4) * 2 + t) * BM + mine;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -646,12 +691,22 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                 if (slot >= 0) {
 #pragma unroll
                     for (int v = 0; v < 8; ++v) prow[(c * 8 + v) * 2 * BM] = make_float4(f[4 * v], f[4 * v + 1], f[4 * v + 2], f[4 * v + 3]);
-                } else if (row < rows) {
+                } else {                                 // into the queries' memory (their products are done), from where whole rows go out
 #pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        *reinterpret_cast<uint4*>(orow + c * 32 + v * 8) = make_uint4(pack_bf16x2(f[8 * v], f[8 * v + 1]), pack_bf16x2(f[8 * v + 2], f[8 * v + 3]),
-                                                                                      pack_bf16x2(f[8 * v + 4], f[8 * v + 5]), pack_bf16x2(f[8 * v + 6], f[8 * v + 7]));
+                    for (int v = 0; v < 4; ++v) {
+                        const int at = c * 4 + v;        // (the piece of the row)
+                        sts16(base_s + t * Q_BYTES + (at >> 3) * (BM * 128) + mine * 128 + (((at & 7) ^ (mine & 7)) << 4), pack_bf16x2(f[8 * v], f[8 * v + 1]),
+                              pack_bf16x2(f[8 * v + 2], f[8 * v + 3]), pack_bf16x2(f[8 * v + 4], f[8 * v + 5]), pack_bf16x2(f[8 * v + 6], f[8 * v + 7]));
+                    }
                 }
+            }
+            if (slot < 0) {
+                __syncwarp();
+                walk(Const<4>{}, [&](int i, int r, int64_t tk, int hd) {
+                    uint32_t x[4];
+                    lds16(spot(i), x);
+                    if (r < rows) *reinterpret_cast<uint4*>(p.O + tk * p.o_st + hd * p.o_sh + piece * 8) = make_uint4(x[0], x[1], x[2], x[3]);
+                });
             }
         }
         if (part_slot >= 0) {
@@ -673,7 +728,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 0) tmem_dealloc(tmem, 512);
+    if (warp == 2) tmem_dealloc(tmem, 512);
 }
 
 template <int D>

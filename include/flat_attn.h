@@ -321,9 +321,9 @@ int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream);
  * lse: optional [total, Hq] fp32, as in flat_attn_params_t.  e4m3 is exact in the half precision of the products.  Queries enter them scaled
  * by a power of two for each row (unrounded where a feature is within 2^-28 of the row's largest); where a sequence has more than 64
  * rows (new tokens times G) keys and values enter scaled relative to the largest page of the sequence and head (unrounded in pages
- * whose scale is within 2^-21 of it); weights are rounded to half precision at 2^9 to 2^15 times their size; sums are fp32.  The keys of long
- * sequences are split over CTAs and joined in a fixed order: same bits every time.  One kernel, or two in a call that may hold sequences
- * of more than 64 rows and others.
+ * whose scale is within 2^-21 of it), otherwise the values' scale, relative to the largest of a part, is multiplied to the weights; weights
+ * are rounded to half precision at 2^9 to 2^15 times their size; sums are fp32.  The keys of long sequences are split over CTAs and joined
+ * in a fixed order: same bits every time.  One kernel, or two in a call that may hold sequences of more than 64 rows and others.
  * workspace: device, at least flat_attn_cache_workspace_bytes(Hq, Hkv, d) bytes on the device of the call, 256-byte aligned, zeroed once by the caller; every call
  * leaves it ready for the next.  Calls that may run at the same time (other streams, captured graphs that overlap) need one each.
  */

@@ -17,12 +17,16 @@
 //
 // What bounds it, d = 128: shared memory's port and the softmax warps together.  A step of both tiles moves 1,024 cycles of operands
 // for the tensor pipe (A of the logits alone 512) and 512 of conversions; its exponentials take 1,010 cycles of the exponent unit;
-// measured 1,920 cycles (softmax 1,270 of work and 330 of waiting for logits).  4,096 queries behind 28,672 tokens, 32 heads on 8:
-// 1,720 us in the first 20 ms of launches (1,200 TFLOP/s), 1,960 at the power cap (1,050; a cuBLAS GEMM 1,639 and 1,396).  d = 64: the exponentials,
-// 550 TFLOP/s.  Tried: the converters' own cp.async (their addresses were half of a step: 587 us against 522 on 128 items), logits
-// of two steps in one product (N = 128, one buffer a tile: 567; d = 64 494 against 466), no polynomial 534 and one in four 521.
+// measured 1,750 cycles (of 1,920 in an earlier form the softmax took 1,270 to work and 330 to wait for logits).  4,096 queries behind
+// 28,672 tokens, 32 heads on 8: 1,580 us in the first 20 ms of launches (1,305 TFLOP/s), 1,830 at the power cap (1,120; a cuBLAS GEMM
+// 1,639 and 1,396).  d = 64: the exponentials, 580 TFLOP/s.  How long a step takes also depends on the code around it: with masked steps in a
+// loop instead of unrolled 128 items of d = 128 take 480 us against 488.  Tried, on 128 items: the converters' own cp.async (their addresses
+// were half of a step: 587 us against 522), logits of two steps in one product (N = 128, one buffer a tile: 567 against 522; d = 64 494
+// against 466), no polynomial 524 and one in sixteen 524 against 512, one in four 513 (d = 64 456 against 459).
+// Where there are few steps: 200 queries of 32 heads on 8 13.8 us, of which the launch 2.5, the deal 1.6, queries and exponents 2, the first
+// step 1.6, the output 2.
 // Items: those of the last round, or all if they are fewer than the SMs, are split along the keys (128 queries, 32 heads on 8, over
-// 32,768 keys: 537 -> 108 us).
+// 32,768 keys: 537 -> 99 us).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -634,8 +634,9 @@ int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_pa
     flat_attn_cache_t q = *c;
     q.status = status_or_library_word(c->status);
     // Rows of a sequence and key head (new tokens times heads a group): up to FEW the warp-level products, whose tiles have sixteen
-    // rows, beyond the tcgen05 form, whose tiles have 128 and which reads the cache once for all of them (us, the one / the other: 12
-    // sequences of 4-32K tokens, 4 key heads, 28 rows 100 / 131, 64 rows 181 / 133; 2 of 1-2K, 8 key heads, 40 rows 16 / 31).  A call
+    // rows, beyond the tcgen05 form, whose tiles have 128 and which reads the cache once for all of them (us, the one / the other, 32
+    // heads on 4, d = 128: 12 sequences of 4-32K tokens, 32 rows 63 / 88, 48 rows 99 / 105, 64 rows 116 / 99; 8 of 4,000, 64 rows 39 / 35;
+    // 2 of 1-2K, 64 rows 17 / 31; one of 16,000, 64 rows 28 / 59).  A call
     // whose longest sequence has more may hold short ones too: both kernels then, each leaving the other's sequences out.
     constexpr int FEW = 64;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -325,7 +325,7 @@ int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream);
  * are rounded to half precision at 2^9 to 2^15 times their size; sums are fp32.  The keys of long sequences are split over CTAs and joined
  * in a fixed order: same bits every time.  One kernel, or two in a call that may hold sequences of more than 64 rows and others.
  * workspace: device, at least flat_attn_cache_workspace_bytes(Hq, Hkv, d) bytes on the device of the call, 256-byte aligned, zeroed once by the caller; every call
- * leaves it ready for the next.  Calls that may run at the same time (other streams, captured graphs that overlap) need one each.
+ * leaves it ready for the next, of any sizes that it is large enough for.  Calls that may run at the same time (other streams, captured graphs that overlap) need one each.
  */
 #define FLAT_CACHE_BAD_PAGE 0xb00
 #define FLAT_CACHE_BAD_LENGTH 0xb01

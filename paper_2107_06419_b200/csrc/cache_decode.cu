@@ -733,7 +733,6 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 namespace {
 size_t most_teams() { return static_cast<size_t>(device_sm_count()) * 3 * WARPS; }     // (three CTAs an SM, a team a warp)
 size_t most_part_rows() { return static_cast<size_t>(device_sm_count()) * 3 * WARPS * 2 * TILE; }    // (two places a team)
-size_t counter_bytes() { return (most_teams() * sizeof(int) + 255) & ~size_t(255); }
 
 template <int D, int RG, int TEAM, bool SMALL>
 int launch(const DecodeArgs& p, cudaStream_t st) {
@@ -758,11 +757,10 @@ int launch_form(const DecodeArgs& p, bool by_warp, cudaStream_t st) {
 }
 }  // namespace
 
-size_t cache_decode_workspace_bytes(int d) {
-    return (counter_bytes() + most_part_rows() * (d + 1) * sizeof(float) + 255) & ~size_t(255);
-}
+size_t cache_decode_counter_bytes() { return (most_teams() * sizeof(int) + 255) & ~size_t(255); }
+size_t cache_decode_part_bytes(int d) { return (most_part_rows() * (d + 1) * sizeof(float) + 255) & ~size_t(255); }
 
-int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int most_rows, bool beside, cudaStream_t st) {
+int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int most_rows, bool beside, int* counters, float* parts, cudaStream_t st) {
     DecodeArgs p{};
     p.c = cache_view(c);
     p.Q = static_cast<const __nv_bfloat16*>(q.Q);
@@ -773,9 +771,8 @@ int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_pa
     p.Hq = q.Hq; p.G = q.Hq / c.Hkv; p.max_new = q.max_new; p.most_rows = most_rows; p.causal = q.causal;
     p.beside = beside;
     p.scale_log2e = q.scale * 1.4426950408889634f;
-    char* w = static_cast<char*>(q.workspace);
-    p.counters = reinterpret_cast<int*>(w);
-    p.part_lse = reinterpret_cast<float*>(w + counter_bytes());
+    p.counters = counters;
+    p.part_lse = parts;
     p.part_o = p.part_lse + most_part_rows();
     const int64_t rows = static_cast<int64_t>(q.max_new) * p.G, most = rows < most_rows ? rows : most_rows;
     const int64_t items = static_cast<int64_t>(c.num_seqs) * c.Hkv * ((most + TILE - 1) / TILE);

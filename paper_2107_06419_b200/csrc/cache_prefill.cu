@@ -767,10 +767,10 @@ int launch_d(const flat_attn_cache_t& c, const PrefillArgs& p, cudaStream_t st) 
 
 }  // namespace
 
-static size_t prefill_counter_bytes() { return (device_sm_count() * 8 * sizeof(int) + 255) & ~size_t(255); }
-size_t cache_prefill_workspace_bytes(int d) { return prefill_counter_bytes() + static_cast<size_t>(device_sm_count()) * 2 * BM * (d + 1) * sizeof(float); }
+size_t cache_prefill_counter_bytes() { return (device_sm_count() * 8 * sizeof(int) + 255) & ~size_t(255); }
+size_t cache_prefill_part_bytes(int d) { return static_cast<size_t>(device_sm_count()) * 2 * BM * (d + 1) * sizeof(float); }
 
-int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int least_rows, void* workspace, cudaStream_t st) {
+int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& q, int least_rows, int* counters, float* parts, cudaStream_t st) {
     PrefillArgs p{};
     p.c = cache_view(c);
     p.Q = static_cast<const __nv_bfloat16*>(q.Q);
@@ -780,9 +780,8 @@ int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_p
     p.total = q.total;
     p.Hq = q.Hq; p.G = q.Hq / c.Hkv; p.max_new = q.max_new; p.least_rows = least_rows; p.causal = q.causal;
     p.sms = device_sm_count();
-    char* w = static_cast<char*>(workspace);
-    p.counters = reinterpret_cast<int*>(w);
-    p.part_lse = reinterpret_cast<float*>(w + prefill_counter_bytes());
+    p.counters = counters;
+    p.part_lse = parts;
     p.part_o = p.part_lse + static_cast<size_t>(p.sms) * 2 * BM;
     p.scale_log2e = q.scale * 1.4426950408889634f;
     return c.d == 64 ? launch_d<64>(c, p, st) : launch_d<128>(c, p, st);

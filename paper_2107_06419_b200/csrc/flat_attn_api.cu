@@ -616,7 +616,7 @@ int flat_attn_cache_append(const flat_attn_cache_t* c, const void* K, const void
 
 size_t flat_attn_cache_workspace_bytes(int Hq, int Hkv, int d) {
     if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || (d != 64 && d != 128)) return 0;
-    return flat::cache_decode_workspace_bytes(d) + flat::cache_prefill_workspace_bytes(d);
+    return flat::cache_decode_counter_bytes() + flat::cache_prefill_counter_bytes() + flat::cache_decode_part_bytes(d) + flat::cache_prefill_part_bytes(d);
 }
 
 int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_params_t* p, void* stream) {
@@ -629,8 +629,11 @@ int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_pa
     const long long in[2] = {p->q_stride_t, p->q_stride_h}, out[2] = {p->o_stride_t, p->o_stride_h}, size[2] = {p->total, p->Hq};
     if (!strides_ok(in, 2, 8) || !strides_ok(out, 2, 8) || !apart(out, size, 2, c->d)) return FLAT_ERR_SHAPE;
     if (!aligned16(p->Q) || !aligned16(p->O) || !aligned(p->workspace, 256) || !aligned(p->lse, 4)) return FLAT_ERR_ALIGN;
-    const size_t behind = flat::cache_decode_workspace_bytes(c->d);
-    if (p->workspace_bytes < behind + flat::cache_prefill_workspace_bytes(c->d)) return FLAT_ERR_WORKSPACE;
+    if (p->workspace_bytes < flat_attn_cache_workspace_bytes(p->Hq, c->Hkv, c->d)) return FLAT_ERR_WORKSPACE;
+    char* const decode_counters = static_cast<char*>(p->workspace);
+    char* const prefill_counters = decode_counters + flat::cache_decode_counter_bytes();
+    char* const decode_parts = prefill_counters + flat::cache_prefill_counter_bytes();
+    char* const prefill_parts = decode_parts + flat::cache_decode_part_bytes(c->d);
     flat_attn_cache_t q = *c;
     q.status = status_or_library_word(c->status);
     // Rows of a sequence and key head (new tokens times heads a group): up to FEW the warp-level products, whose tiles have sixteen
@@ -643,12 +646,12 @@ int flat_attn_cache_fwd(const flat_attn_cache_t* c, const flat_attn_cache_fwd_pa
     const bool many = static_cast<int64_t>(p->max_new) * (p->Hq / c->Hkv) > FEW, few = !many || c->num_seqs > 1;
     int launches = 0;
     if (many) {
-        const int r = flat::launch_cache_prefill(q, *p, few ? FEW : 0, static_cast<char*>(p->workspace) + behind, st);
+        const int r = flat::launch_cache_prefill(q, *p, few ? FEW : 0, reinterpret_cast<int*>(prefill_counters), reinterpret_cast<float*>(prefill_parts), st);
         if (r != FLAT_OK) return r;
         ++launches;
     }
     if (few) {
-        const int r = flat::launch_cache_decode(q, *p, FEW, many, st);
+        const int r = flat::launch_cache_decode(q, *p, FEW, many, reinterpret_cast<int*>(decode_counters), reinterpret_cast<float*>(decode_parts), st);
         if (r != FLAT_OK) return r;
         ++launches;
     }

@@ -118,11 +118,15 @@ int launch_rope(const flat_attn_rope_params_t& p, bool back, cudaStream_t st);
 // rows, new tokens times query heads a key head; cache_prefill.cu: the others).
 int launch_cache_append(const flat_attn_cache_t& c, const void* K, const void* V, int64_t total, long long k_st, long long k_sh,
                         long long v_st, long long v_sh, int max_new, cudaStream_t st);
-int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& p, int most_rows, bool beside, cudaStream_t st);   // (beside: behind the other)
-int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& p, int least_rows, void* workspace, cudaStream_t st);
-// Their workspaces: the decode kernel's first (a multiple of 256 bytes), the other's behind it.
-size_t cache_decode_workspace_bytes(int d);
-size_t cache_prefill_workspace_bytes(int d);
+int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& p, int most_rows, bool beside, int* counters, float* parts,
+                        cudaStream_t st);                // (beside: behind the other)
+int launch_cache_prefill(const flat_attn_cache_t& c, const flat_attn_cache_fwd_params_t& p, int least_rows, int* counters, float* parts, cudaStream_t st);
+// Their workspace, multiples of 256 bytes: the counters of both, which lie at the same places whatever d is (a call leaves them at 0 for calls of
+// either d), and then what a call leaves nothing in: the parts of split items.
+size_t cache_decode_counter_bytes();
+size_t cache_prefill_counter_bytes();
+size_t cache_decode_part_bytes(int d);
+size_t cache_prefill_part_bytes(int d);
 int launch_wait_timeout_selftest(int32_t* status, cudaStream_t st);
 int launch_exp2_poly_selftest(const float* x, float* y, int n, cudaStream_t st);
 // Tensor-core versions of the baseline's two contractions (bf16, d in {64,128}, Nk % 8 == 0).

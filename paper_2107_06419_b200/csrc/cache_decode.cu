@@ -101,6 +101,11 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ void sts16(uint32_t addr, const uint32_t (&r)[4]) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+// The NaN among four e4m3 (0x7f and 0xff), as whole bytes.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 255u; }
 // The 8 x 8 matrix of half-precision pairs (lane: row lane / 4, columns 2 (lane % 4), + 1), transposed.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     uint32_t r;
@@ -123,9 +128,28 @@ __device__ __forceinline__ float two_to(int e) {         // 2^e for any e: 0 bel
     return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
 }
 
+// The values of the keys key0 .. key1 - 1 that are NaN, for each row (of `rows`, from row0 of the sequence's on) that sees the key, by a warp: store(row,
+// feature).  Key j is seen from token j - before on.
+template <int D, typename Store>
+__device__ __noinline__ void put_nan(const CacheView& cv, const int32_t* table, int h, int key0, int key1, int before, int row0, int rows, int G, Store store) {
+    const int at = (threadIdx.x & 31) * 4;               // the lane's four features
+    for (int key = key0; key < key1 && at < D; ++key) {
+        const int id = table[key >> cv.page_shift];
+        if (id < 0 || id >= cv.num_pages) continue;
+        const int64_t token = ((static_cast<int64_t>(id) * cv.Hkv + h) << cv.page_shift) + (key & (cv.page - 1));
+        const uint32_t gone = nan_bytes(*reinterpret_cast<const uint32_t*>(cv.v + token * D + at));
+        if (!gone) continue;
+        for (int row = 0; row < rows; ++row)
+            if ((row0 + row) / G >= key - before)
+                for (int e = 0; e < 4; ++e)
+                    if (gone >> (8 * e) & 1) store(row, at + e);
+    }
+}
+
 // TEAM: warps of a team (4 or 1).  RG: row groups of eight in a tile (1: no sequence has more than eight rows).  SMALL: pages of less
-// than a chunk.
-template <int D, int RG, int TEAM, bool SMALL>
+// than a chunk.  DRAFTS: rows may see fewer keys than their sequence has (without what that takes, one sequence of 2,000 tokens 8.8 us, with it
+// 9.1; only one row group has both forms).
+template <int D, int RG, int TEAM, bool SMALL, bool DRAFTS>
 __global__ void __launch_bounds__(THREADS, CTAS(RG, TEAM))
 cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
     constexpr int CH = HALF_BYTES / D;                   // tokens of a chunk: 32 (d = 128) or 64
@@ -383,6 +407,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
         // o[x][r]: features 16 x + g (0, 1) and 16 x + g + 8 (2, 3) of the rows 8 r + 2 t and 8 r + 2 t + 1
         float o[PIECES][RG][4], m[RG][2], l[RG][2];
         int E = -1000;                                   // o is in units of 2^E
+        bool cleaned = false;                            // values that are NaN and not for every row have been taken out (the same in all lanes)
 #pragma unroll
         for (int r = 0; r < RG; ++r) {
 #pragma unroll
@@ -405,6 +430,29 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             for (int i = 0; i < STAGES - 1; ++i) place[i] = place[i + 1];
             place[STAGES - 1] = load_place(k + STAGES);
             const uint32_t ks = ring + st * CHUNK_BYTES, vs = ks + HALF_BYTES;
+            // A weight of 0 would not keep the NaN of a value from a row that does not see it: out they go where some row does not, and
+            // into the outputs of those that do at the end.  (Drafts, one or two chunks of an item.)
+            if (DRAFTS && nmin < sp.len && key0 + CH > nmin) {
+                bool found = false;
+#pragma unroll 1
+                for (int i = lane; i < HALF_BYTES / 16; i += 32) {
+                    if (key0 + i / PIECES < nmin) continue;
+                    uint32_t w[4], any = 0;
+                    lds16(vs + i * 16, w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t gone = nan_bytes(w[e]);
+                        any |= gone;
+                        w[e] &= ~gone;
+                    }
+                    if (any) {
+                        sts16(vs + i * 16, w);
+                        found = true;
+                    }
+                }
+                if (__any_sync(0xffffffffu, found)) cleaned = true;
+                __syncwarp();
+            }
             // base-2 logits; keys that a row does not see take no part
             const bool masked = key0 + CH > nmin || bad != 0;
             float uk[NT], wv[NT];                        // of sixteen keys: their scale; what their weights are multiplied by for their values' scale
@@ -596,6 +644,13 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
             *reinterpret_cast<uint2*>(p.O + (sp.q0 + tok) * p.o_st + head * p.o_sh + col) = w;
             if (p.lse && col == 0) p.lse[static_cast<long long>(sp.q0 + tok) * p.Hq + head] = lse2 * 0.6931471805599453f;
         };
+        auto put_cleaned = [&](auto store) {             // the NaN that were taken out of this warp's chunks, into what it has written
+            __syncwarp();
+            for (int k = 0; k < count; ++k) {
+                const int key0 = (a0 + member + k * TEAM) * CH;
+                put_nan<D>(cv, table, h, max(key0, nmin), min(key0 + CH, sp.len), sp.len - sp.n, tile * TILE, rows, p.G, store);
+            }
+        };
         if (TEAM == 1) {
 #pragma unroll
             for (int r = 0; r < RG; ++r)
@@ -618,6 +673,12 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     if (g == 0 && !whole) p.part_lse[slot * TILE + row] = lg[r][y];
                     if (g == 0 && whole && p.lse) p.lse[static_cast<long long>(sp.q0 + tok) * p.Hq + head] = lg[r][y] * 0.6931471805599453f;
                 }
+            if (cleaned && whole)
+                put_cleaned([out = p.O + sp.q0 * p.o_st + h * p.G * p.o_sh, o_st = p.o_st, o_sh = p.o_sh, G = p.G, row0 = tile * TILE](int row, int feature) {
+                    const int tok = (row0 + row) / G;
+                    out[tok * o_st + (row0 + row - tok * G) * o_sh + feature] = __ushort_as_bfloat16(0x7fff);
+                });
+            else if (cleaned) put_cleaned([out = p.part_o + slot * TILE * D](int row, int feature) { out[row * D + feature] = __int_as_float(0x7fffffff); });
         } else {
             // the team's warps join through the memory of their rings
             __syncthreads();
@@ -634,6 +695,7 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
                     }
                     if (g == 0) warp_lse[warp][row] = lg[r][y];
                 }
+            if (cleaned) put_cleaned([out = joined + warp * 8 * RG * JOIN](int row, int feature) { out[row * JOIN + feature] = __int_as_float(0x7fffffff); });
             __syncthreads();
             for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
                 const int row = i / (D / 4), col = i % (D / 4) * 4;
@@ -734,9 +796,9 @@ namespace {
 size_t most_teams() { return static_cast<size_t>(device_sm_count()) * 3 * WARPS; }     // (three CTAs an SM, a team a warp)
 size_t most_part_rows() { return static_cast<size_t>(device_sm_count()) * 3 * WARPS * 2 * TILE; }    // (two places a team)
 
-template <int D, int RG, int TEAM, bool SMALL>
+template <int D, int RG, int TEAM, bool SMALL, bool DRAFTS>
 int launch(const DecodeArgs& p, cudaStream_t st) {
-    if (!ensure_dynamic_smem<cache_decode_kernel<D, RG, TEAM, SMALL>>(SMEM_BYTES(D, RG, TEAM))) return FLAT_ERR_CUDA;
+    if (!ensure_dynamic_smem<cache_decode_kernel<D, RG, TEAM, SMALL, DRAFTS>>(SMEM_BYTES(D, RG, TEAM))) return FLAT_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(device_sm_count() * CTAS(RG, TEAM));
     cfg.blockDim = dim3(THREADS);
@@ -747,13 +809,18 @@ int launch(const DecodeArgs& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, cache_decode_kernel<D, RG, TEAM, SMALL>, p) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, cache_decode_kernel<D, RG, TEAM, SMALL, DRAFTS>, p) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA;
 }
-template <int D, int RG>
+template <int D, int RG, bool DRAFTS>
 int launch_form(const DecodeArgs& p, bool by_warp, cudaStream_t st) {
     const bool small = p.c.page < HALF_BYTES / D;
-    if (by_warp) return small ? launch<D, RG, 1, true>(p, st) : launch<D, RG, 1, false>(p, st);
-    return small ? launch<D, RG, WARPS, true>(p, st) : launch<D, RG, WARPS, false>(p, st);
+    if (by_warp) return small ? launch<D, RG, 1, true, DRAFTS>(p, st) : launch<D, RG, 1, false, DRAFTS>(p, st);
+    return small ? launch<D, RG, WARPS, true, DRAFTS>(p, st) : launch<D, RG, WARPS, false, DRAFTS>(p, st);
+}
+template <int D>
+int launch_d(const DecodeArgs& p, int64_t most, bool by_warp, cudaStream_t st) {
+    if (most > 8) return launch_form<D, 2, true>(p, by_warp, st);
+    return p.causal && p.max_new > 1 ? launch_form<D, 1, true>(p, by_warp, st) : launch_form<D, 1, false>(p, by_warp, st);
 }
 }  // namespace
 
@@ -777,8 +844,7 @@ int launch_cache_decode(const flat_attn_cache_t& c, const flat_attn_cache_fwd_pa
     const int64_t rows = static_cast<int64_t>(q.max_new) * p.G, most = rows < most_rows ? rows : most_rows;
     const int64_t items = static_cast<int64_t>(c.num_seqs) * c.Hkv * ((most + TILE - 1) / TILE);
     const bool by_warp = items >= static_cast<int64_t>(most_teams());
-    if (c.d == 64) return most <= 8 ? launch_form<64, 1>(p, by_warp, st) : launch_form<64, 2>(p, by_warp, st);
-    return most <= 8 ? launch_form<128, 1>(p, by_warp, st) : launch_form<128, 2>(p, by_warp, st);
+    return c.d == 64 ? launch_d<64>(p, most, by_warp, st) : launch_d<128>(p, most, by_warp, st);
 }
 
 }  // namespace flat

@@ -56,3 +56,55 @@ def test_one_workspace_for_both_head_sizes(api, sms):
         check_call(api, gen, w, [140], [3000], 2, 2, 32, 128, times=2)
         check_call(api, gen, w, [1] * seqs, lens, 1, 8, 16, 64)
     assert int(w[:20 * 4 * sms].sum()) == 0              # the counters of both kernels are at its beginning, and 0 again
+
+
+# ---------------------------------------------------------------- entries that are not numbers
+
+def attend_with_nan(api, gen, new, lens, G, page, d, causal):
+    """NaN among the keys and values of four heads; a row is NaN where it sees a NaN key, a feature of it where it sees a NaN value, and
+    nothing else is (0: values of new tokens, 1: a key of a new token, 2: keys of cached tokens, one in eight, 3: values of the
+    first and last tokens)."""
+    Hkv, cu = 4, ref.offsets(new)
+    k, v, ke, ve, table = ref.make_cache(gen, lens, Hkv, page, d, "cuda")
+    clean = [k.clone(), v.clone()]
+    T = cu[-1]
+    rows, cells = torch.zeros(T, G * Hkv, dtype=torch.bool), torch.zeros(T, G * Hkv, d, dtype=torch.bool)
+    for s, (n, m) in enumerate(zip(new, lens)):
+        at = m - n
+        marks = [(1, h, j, f) for h, j, f in [(0, at, 3), (0, at + n // 2, d - 1), (0, m - 1, 0), (3, min(5, m - 1), 17), (3, m - 1, 40)]]
+        marks += [(0, 1, at + (n - 1) // 2, 9)] + [(0, 2, j, (7 * j) % d) for j in range(67, at, 8 * (1 + at // 100))]
+        for which, h, j, f in marks:
+            p, r = int(table[s, j // page]), j % page
+            (k, v)[which].view(torch.uint8)[p, h, r, f] = 0xFF if (j + f) % 2 else 0x7F
+            clean[which].view(torch.uint8)[p, h, r, f] = 0
+            first = cu[s] + (max(0, j - at) if causal else 0)              # the first row that sees key j
+            for g in range(h * G, (h + 1) * G):
+                if which:
+                    cells[first:cu[s + 1], g, f] = True
+                else:
+                    rows[first:cu[s + 1], g] = True
+    rows, cells = rows.cuda(), (cells | rows[..., None]).cuda()
+    Q = torch.randn(T, G * Hkv, d, generator=gen).to(torch.bfloat16).cuda()
+    O, lse = torch.full_like(Q, 7.0), torch.full((T, G * Hkv), 7.0, device="cuda")
+    api.flat_attn_cache_fwd(Q, O, k, v, ke, ve, table, ints(cu), ints(lens), max(new), 0.1, workspace(api, G * Hkv, Hkv, d), causal=causal, lse=lse)
+    torch.cuda.synchronize()
+    R, L, A, B = ref.attention(Q, *clean, ke, ve, table, cu, lens, 0.1, causal)
+    assert torch.equal(torch.isnan(O), cells), (int((torch.isnan(O) & ~cells).sum()), int((cells & ~torch.isnan(O)).sum()))
+    assert torch.equal(torch.isnan(lse), rows)
+    ref.check_attention(torch.where(cells, R, O.double()), torch.where(rows, L, lse.double()), (R, L, A, B), d)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("G,new,lens", [(2, [4, 3, 1], [300, 77, 1000]), (7, [5, 2], [1500, 40]), (1, [64], [64]), (8, [8, 1], [8, 500])])
+def test_nan_reaches_what_sees_it(api, d, page, causal, G, new, lens):
+    attend_with_nan(api, torch.Generator().manual_seed(sum(lens) + G), new, lens, G, page, d, causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page,G,n", [(16, 2, 4), (64, 4, 4)])
+def test_nan_where_items_are_dealt_to_single_warps(api, sms, d, page, G, n):
+    seqs = -(-12 * sms // 4)
+    lens = [n + 53 * s % 300 for s in range(seqs)]
+    attend_with_nan(api, torch.Generator().manual_seed(22), [n] * seqs, lens, G, page, d, True)

@@ -45,5 +45,8 @@ __device__ __forceinline__ bool read_page(const CacheView& c, int s, int index, 
     return false;
 }
 
+// The NaN among four e4m3 (0x7f and 0xff), as whole bytes.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 255u; }
+
 }  // namespace cache
 }  // namespace flat

@@ -104,8 +104,6 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 __device__ __forceinline__ void sts16(uint32_t addr, const uint32_t (&r)[4]) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-// The NaN among four e4m3 (0x7f and 0xff), as whole bytes.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 255u; }
 // The 8 x 8 matrix of half-precision pairs (lane: row lane / 4, columns 2 (lane % 4), + 1), transposed.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     uint32_t r;

@@ -206,9 +206,9 @@ __device__ __forceinline__ void join_rows(const PrefillArgs& p, int slot0, int p
 }
 
 // What a CTA works on: sequence, its first query, length, tokens before the new ones; head; rows of the sequence and the slab's first;
-// keys that the slab sees; the part's steps; whether the second tile has rows.
+// keys that the slab sees, and those that all of its rows see; the part's steps; whether the second tile has rows.
 struct Work {
-    int s, q0, len, before, h, rows, row0, n, j0, nsteps, two;
+    int s, q0, len, before, h, rows, row0, n, n_all, j0, nsteps, two;
 };
 constexpr int GROUPS = 32;                               // groups of sixteen tokens that are looked up at a time: eight steps
 
@@ -223,6 +223,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + LY::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     __shared__ int top_exp[2], any_bad;
+    __shared__ volatile int cleaned;                     // values that are NaN and not for every row have been taken out
     // an item in parts: the part's place in the workspace (-1: the item is in one part), its index among them, their number, the item's place
     __shared__ int part_slot, part_index, part_count, part_item;
     __shared__ Work work;                                // (what the roles need of the mapping below: read again, not kept in registers)
@@ -235,7 +236,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                                 : i < LY::K_EMPTY || (i >= LY::V_FULL && i < LY::V_EMPTY) || (i >= LY::P_FULL && i < LY::PV_DONE) || i >= LY::SCALE_EMPTY ? 4
                                 : (i >= LY::K_EMPTY && i < LY::V_FULL) || (i >= LY::V_EMPTY && i < LY::S_FULL) ? 2 : 1);
         *abort_flag = 0;
-        top_exp[0] = top_exp[1] = any_bad = 0;
+        top_exp[0] = top_exp[1] = any_bad = cleaned = 0;
         fence_mbar_init();
     }
     if (warp == 2) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
@@ -325,7 +326,8 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     if (part >= parts) return;
     if (lane == 0) {
         const int j0 = all_steps * part / parts;
-        work = Work{s, sp.q0, sp.len, sp.len - sp.n, h, rows, row0, n, j0, all_steps * (part + 1) / parts - j0, rows - row0 > BM};
+        const int n_all = p.causal ? min(row0 / p.G + 1 + sp.len - sp.n, n) : n;
+        work = Work{s, sp.q0, sp.len, sp.len - sp.n, h, rows, row0, n, n_all, j0, all_steps * (part + 1) / parts - j0, rows - row0 > BM};
         part_slot = parts == 1 ? -1 : each ? unit : unit - whole;
         part_index = part;
         part_count = parts;
@@ -401,6 +403,20 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
             if (lane == 0) {
                 mbar_arrive(&bars[LY::K_FULL + j % KS]);
                 mbar_arrive(&bars[LY::RAW_EMPTY + j % LS]);      // (all of it is in registers)
+            }
+            // (a weight of 0 would not keep a NaN from the rows that do not see its key: the rows that do get it at the end)
+            const int n_all = work.n_all;
+            if ((work.j0 + j + 1) * BN > n_all) {
+                uint32_t any = 0;
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t gone = key0 + j * BN + 32 * (i & 1) >= n_all ? nan_bytes(v[i][e]) : 0u;
+                        any |= gone;
+                        v[i][e] &= ~gone;
+                    }
+                if (any) cleaned = 1;
             }
             wait(LY::V_EMPTY + j % VS, ((j / VS) & 1) ^ 1, 0xb11);
             if (!ok) break;
@@ -706,6 +722,23 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                         const int at = c * 4 + v;        // (the piece of the row)
                         sts16(base_s + t * Q_BYTES + (at >> 3) * (BM * 128) + mine * 128 + (((at & 7) ^ (mine & 7)) << 4), pack_bf16x2(f[8 * v], f[8 * v + 1]),
                               pack_bf16x2(f[8 * v + 2], f[8 * v + 3]), pack_bf16x2(f[8 * v + 4], f[8 * v + 5]), pack_bf16x2(f[8 * v + 6], f[8 * v + 7]));
+                    }
+                }
+            }
+            if (cleaned) {                               // the values that were taken out, into the row's own place of what was just written
+                const volatile Work& w = work;           // (read again: nothing of this is kept in registers through the steps)
+                const int r = w.row0 + t * BM + mine, key1 = r < w.rows ? min(p.causal ? r / p.G + 1 + w.before : w.n, (w.j0 + w.nsteps) * BN) : 0;
+#pragma unroll 1
+                for (int key = max(w.n_all, w.j0 * BN); key < key1; ++key) {
+                    const int id = cv.table[static_cast<int64_t>(w.s) * cv.max_pages + (key >> cv.page_shift)];
+                    if (id < 0 || id >= cv.num_pages) continue;
+                    const uint8_t* v = cv.v + (((static_cast<int64_t>(id) * cv.Hkv + w.h) << cv.page_shift) + (key & (cv.page - 1))) * D;
+#pragma unroll 1
+                    for (int f = 0; f < D; ++f) {
+                        if ((v[f] & 0x7f) != 0x7f) continue;
+                        if (slot >= 0) reinterpret_cast<float*>(prow + (f >> 2) * 2 * BM)[f & 3] = __int_as_float(0x7fffffff);
+                        else asm volatile("st.shared.u16 [%0], %1;" ::"r"(base_s + t * Q_BYTES + (f >> 6) * (BM * 128) + mine * 128 + (((f >> 3 & 7) ^ (mine & 7)) << 4) + (f & 7) * 2),
+                                          "h"(static_cast<uint16_t>(0x7fff)) : "memory");
                     }
                 }
             }

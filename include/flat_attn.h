@@ -317,7 +317,8 @@ int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream);
  *
  * flat_attn_cache_fwd: Q, O [total, Hq, d] bf16 (strides as above), Hq = G * Hkv: query head h reads key head h / G, G <= 128.  causal = 1:
  * query i of n sees the keys j <= i + length - n; 0: all of its sequence.  O = 0 (and lse = -inf) for a row whose keys are all left out.
- * Cache entries of a sequence must be finite; what lies behind its length in its last page is ignored, NaN included.
+ * NaN in the cache reach what sees them and nothing else: a row whose keys hold one is NaN, lse too, and a value's NaN is one in its feature of the rows that
+ * see the key.  What lies behind a sequence's length in its last page is ignored, NaN included.
  * lse: optional [total, Hq] fp32, as in flat_attn_params_t.  e4m3 is exact in the half precision of the products.  Queries enter them scaled
  * by a power of two for each row (unrounded where a feature is within 2^-28 of the row's largest); where a sequence has more than 64
  * rows (new tokens times G) keys and values enter scaled relative to the largest page of the sequence and head (unrounded in pages

@@ -84,7 +84,7 @@ __device__ __forceinline__ float two_to(int e) {         // 2^e for any e: 0 bel
 }
 
 // Of sixteen logits p_i = 2^(s_i * unit + neg_m), rounded to half precision into eight TMEM columns at `p_addr`; the fp32 sums of the
-// unrounded p go to sum0 and sum1.  TAIL: only the first `nvalid` take part.
+// unrounded p go to sum0 and sum1 (a NaN logit makes them NaN or, through the polynomial, 2^126: the step is redone then).  TAIL: only the first `nvalid` take part.
 template <bool TAIL>
 __device__ __forceinline__ void exp16(const uint32_t* s, uint64_t unit2, uint64_t neg_m2, uint32_t p_addr, int nvalid, uint64_t& sum0, uint64_t& sum1) {
     uint32_t pk[8];
@@ -93,7 +93,7 @@ __device__ __forceinline__ void exp16(const uint32_t* s, uint64_t unit2, uint64_
     for (int i = 0; i < 16; i += 2) unpack2(fma2(pack2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), unit2, neg_m2), p[i], p[i + 1]);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        p[i] = !TAIL && (i & 7) == POLY_LANE ? ex2_poly(p[i]) : ex2_approx(p[i]);
+        p[i] = !TAIL && (i & 7) == POLY_LANE ? ex2_poly<true>(p[i]) : ex2_approx(p[i]);
         if (TAIL && i >= nvalid) p[i] = 0.f;
     }
 #pragma unroll

@@ -112,9 +112,13 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // [-126, 126] so that the exponent arithmetic cannot wrap (the cubic lies in [0.70, 1.42], biased
 // exponent 126 or 127, so r >= -126 keeps the field at 0 or above): below, the result is a
 // denormal of about 2^-126 (as good as 0 next to a row maximum of order 1); above, it is 2^126,
-// which trips the caller's overflow check exactly like the ex2 unit's +inf would.
+// which trips the caller's overflow check exactly like the ex2 unit's +inf would.  NaN: as the lowest number, or (NAN_HIGH) the highest, so that
+// the check sees them too.
+template <bool NAN_HIGH = false>
 __device__ __forceinline__ float ex2_poly(float x) {
-    x = fminf(fmaxf(x, -126.f), 126.f);
+    if (NAN_HIGH) asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(-126.f));
+    else x = fmaxf(x, -126.f);
+    x = fminf(x, 126.f);
     const float t = x + 12582912.f;                    // 1.5 * 2^23: the low mantissa bits now hold round(x)
     const float r = t - 12582912.f;
     const float f = x - r;

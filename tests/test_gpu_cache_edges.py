@@ -98,7 +98,7 @@ def attend_with_nan(api, gen, new, lens, G, page, d, causal):
 @pytest.mark.parametrize("page", [16, 128])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("G,new,lens", [(2, [4, 3, 1], [300, 77, 1000]), (7, [5, 2], [1500, 40]), (1, [64], [64]), (8, [8, 1], [8, 500]), (1, [300], [1900]),
-                                        (3, [150, 3, 1], [700, 200, 64])])
+                                        (2, [200, 90], [400, 90]), (3, [150, 3, 1], [700, 200, 64])])
 def test_nan_reaches_what_sees_it(api, d, page, causal, G, new, lens):
     attend_with_nan(api, torch.Generator().manual_seed(sum(lens) + G), new, lens, G, page, d, causal)
 

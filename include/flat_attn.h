@@ -296,7 +296,7 @@ int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream);
  * A cache of keys and values in 8 bits, in pages, and attention over it (the same operators as flat_attn_varlen_fwd: Section 2
  * steps 2-4 sequence by sequence; the paper has no counterpart for the cache).
  *   k_cache, v_cache : [num_pages, Hkv, page, d] e4m3 (no infinities; 0x7f and 0xff are NaN)
- *   k_exp, v_exp     : [num_pages, Hkv] bytes: the values of a page and head are the e4m3 numbers times 2^(exp - 127)
+ *   k_exp, v_exp     : [num_pages, Hkv] bytes, 10 to 247: the values of a page and head are the e4m3 numbers times 2^(exp - 127)
  *   page_table       : [num_seqs, max_pages] int32, row s the pages of sequence s in order; entries behind its length are not read
  *   cu_seqlens       : [num_seqs + 1] int32: sequence s owns the new tokens cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (its queries, or the
  *                      keys and values to append); may own none.  Tokens behind the last sequence are left alone.

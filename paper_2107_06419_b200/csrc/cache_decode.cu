@@ -622,14 +622,15 @@ cache_decode_kernel(const __grid_constant__ DecodeArgs p) {
 
         // ------------------------------------------------------------ normalised outputs and log-sums of this warp's keys
         float lg[RG][2];
+        const float scale = two_to(E - 127);             // (multiplied by itself: over the sum it could lie below the least normal number)
 #pragma unroll
         for (int r = 0; r < RG; ++r)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const float sum = column_sum(l[r][y]), inv = sum > 0.f ? two_to(E - 127) / sum : sum == sum ? 0.f : sum;
+                const float sum = column_sum(l[r][y]), inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
                 lg[r][y] = sum > 0.f ? m[r][y] - WEIGHT_SHIFT + log2f(sum) : sum == sum ? -INFINITY : sum;
 #pragma unroll
-                for (int i = 0; i < PIECES; ++i) { o[i][r][y] *= inv; o[i][r][2 + y] *= inv; }
+                for (int i = 0; i < PIECES; ++i) { o[i][r][y] = o[i][r][y] * inv * scale; o[i][r][2 + y] = o[i][r][2 + y] * inv * scale; }
             }
         const bool whole = parts == 1;
         auto finish = [&](int row, int col, float4 v, float lse2) {     // four features of the item's row

@@ -698,7 +698,8 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
         }
         if (ok) ok = warp_wait(my_bars + 64 + 8 * ((nsteps - 1) & 1), ((nsteps - 1) >> 1) & 1, abort_s, cv.status, 0xb34 + t);
         if (ok) {
-            const float inv = l > 0.f ? two_to(top_exp[1] - 127 - LIFT) / l : l == l ? 0.f : l;
+            // (the scale by itself: over the sum it could lie below the least normal number)
+            const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l, scale = two_to(top_exp[1] - 127 - LIFT);
             const float lse2 = l > 0.f ? m_ref - SHIFT + log2f(l) : l == l ? -INFINITY : l;
             const int slot = part_slot;
             if (slot >= 0) p.part_lse[(slot * 2 + t) * BM + mine] = lse2;
@@ -712,7 +713,7 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                 tc_wait_ld();
                 float f[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]) * inv;
+                for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]) * inv * scale;
                 if (slot >= 0) {
 #pragma unroll
                     for (int v = 0; v < 8; ++v) prow[(c * 8 + v) * 2 * BM] = make_float4(f[4 * v], f[4 * v + 1], f[4 * v + 2], f[4 * v + 3]);

@@ -109,3 +109,47 @@ def test_nan_where_items_are_dealt_to_single_warps(api, sms, d, page, G, n):
     seqs = -(-12 * sms // 4)
     lens = [n + 53 * s % 300 for s in range(seqs)]
     attend_with_nan(api, torch.Generator().manual_seed(22), [n] * seqs, lens, G, page, d, True)
+
+
+# ---------------------------------------------------------------- scales at the ends of the range
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 5, 200])
+@pytest.mark.parametrize("keys,values,size", [((112, 124), (10, 22), 1.0), ((10, 14), (112, 124), 2.0 ** 111), ((112, 124), (225, 238), 1.0)])
+def test_least_and_largest_scales(api, d, new, keys, values, size):
+    """Values down to the least scale that an append writes (whose numbers bf16 still holds), keys too (under large queries)."""
+    gen = torch.Generator().manual_seed(23)
+    lens, cu, Hkv, G, page = [700, 20000], ref.offsets([new, new]), 2, 2, 32
+    k, v, ke, ve, table = ref.make_cache(gen, lens, Hkv, page, d, "cuda")
+    ke.copy_(torch.randint(*keys, ke.shape, generator=gen).to(torch.uint8))
+    ve.copy_(torch.randint(*values, ve.shape, generator=gen).to(torch.uint8))
+    Q = (torch.randn(cu[-1], G * Hkv, d, generator=gen) * size).to(torch.bfloat16).cuda()
+    O, lse = torch.empty_like(Q), torch.empty(cu[-1], G * Hkv, device="cuda")
+    api.flat_attn_cache_fwd(Q, O, k, v, ke, ve, table, ints(cu), ints(lens), new, 0.1, workspace(api, G * Hkv, Hkv, d), causal=True, lse=lse)
+    torch.cuda.synchronize()
+    R, L, A, B = ref.attention(Q, k, v, ke, ve, table, cu, lens, 0.1, True)
+    up = 2.0 ** (117 - (values[0] + values[1]) // 2)     # (a power of two: the bounds count relative to values of about 1)
+    ref.check_attention(O.double() * up, lse, (R * up, L, A * up, B), d)
+
+
+@pytest.mark.parametrize("new,longest", [(1, 1 << 26), (70, 1 << 24)])
+def test_least_scale_over_many_keys(api, new, longest):
+    """Values at the least scale, of a page that the table names again and again: weights add up to 2^35 and more, and the outputs are the page's."""
+    d, page = 64, 16
+    gen = torch.Generator().manual_seed(28)
+    k, v, ke, ve, _ = ref.make_cache(gen, [page], 1, page, d, "cuda", spare=0, exps=(114, 116))
+    ve.fill_(10)
+    table = torch.zeros(1, longest // page, dtype=torch.int32, device="cuda")
+    Q = torch.randn(new, 1, d, generator=gen).to(torch.bfloat16).cuda()
+    O, lse = torch.empty_like(Q), torch.empty(new, 1, device="cuda")
+    api.flat_attn_cache_fwd(Q, O, k, v, ke, ve, table, ints([0, new]), ints([longest]), new, 0.125, workspace(api, 1, 1, d), causal=False, lse=lse)
+    torch.cuda.synchronize()
+    R, L, A, B = ref.attention(Q, k, v, ke, ve, [[0]], [0, new], [page], 0.125, False)
+    # (long sums: half a step, 2^-24, for each of the weights that a lane adds up and 2^-23 for each sixteen keys, at most 2^24 / 16 keys of
+    # a part: one token, 2^26 keys in more than 64 parts of four warps, eight lanes a row each; 70 tokens, a thread a row and 64 keys at a time)
+    keys = longest / (256 if new == 1 else 16)
+    more = keys / (8 if new == 1 else 64) * 2.0 ** -24 + keys / 16 * 2.0 ** -23
+    logits = d * 2.0 ** -24 * B
+    err, up = (O.double() - R).abs(), 2.0 ** 117
+    assert (err * up <= (2.0 ** -8 * R.abs() + (2.0 ** -10 + 2 * logits[..., None] + more) * A) * up).all(), float((err / A).max())
+    assert ((lse.double() - (L + math.log(longest // page))).abs() <= logits + 2.0 ** -18 * (1 + 20) + more).all()

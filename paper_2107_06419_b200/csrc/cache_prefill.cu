@@ -474,8 +474,8 @@ cache_prefill_kernel(const __grid_constant__ PrefillArgs p) {
                     }
                 }
             }
-            if (!ok)                                     // (copies in flight end before the CTA does)
-                for (int j = issued > LS ? issued - LS : 0; j < issued; ++j) drain_wait(&bars[LY::RAW_FULL + j % LS], (j / LS) & 1);
+            // (copies in flight end before the CTA does, whoever gave up waiting for them)
+            for (int j = issued > LS ? issued - LS : 0; j < issued; ++j) drain_wait(&bars[LY::RAW_FULL + j % LS], (j / LS) & 1);
         } else if (warp <= 9) {
             // -------------------------------------------------------- MMA issuer of tile t (whole warp walks, one lane issues)
             const int t = warp - 8;

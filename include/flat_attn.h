@@ -301,12 +301,14 @@ int flat_attn_rope_bwd(const flat_attn_rope_params_t* p, void* stream);
  *   cu_seqlens       : [num_seqs + 1] int32: sequence s owns the new tokens cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (its queries, or the
  *                      keys and values to append); may own none.  Tokens behind the last sequence are left alone.
  *   seq_lens         : [num_seqs] int32: tokens of sequence s, the new ones (its last) included
- * All are device memory, caller-owned.  page in {16, 32, 64, 128}, d in {64, 128} (FLAT_ERR_UNSUPPORTED); num_pages * Hkv < 2^31, max_pages * page <= 2^30,
+ * All are device memory, caller-owned.  page in {16, 32, 64, 128}, d in {64, 128} (FLAT_ERR_UNSUPPORTED); Hkv <= 65535, num_pages * Hkv < 2^31, max_pages * page <= 2^30,
  * num_seqs * Hkv * max_pages * page <= 2^34.  16-byte aligned, the
- * int32 arrays 4-byte.  max_new >= the new tokens of every sequence (it sizes the grid).
+ * int32 arrays 4-byte.  total >= 1 (rows of K, V, Q); max_new: at least the new tokens of every sequence, at most total (FLAT_ERR_SHAPE).  It sizes the grid
+ * and chooses the kernels' forms: a number far above the largest is slower.
  * What the device finds wrong in page_table, cu_seqlens and seq_lens faults nothing: a sequence whose offsets do not lie in
  * 0 .. total, or that has more new tokens than max_new or than its length, or a length beyond max_pages * page, is left out (FLAT_CACHE_BAD_LENGTH in
- * `status`, its outputs unwritten); a page index outside 0 .. num_pages - 1 is left out with its tokens (FLAT_CACHE_BAD_PAGE).
+ * `status`, its outputs unwritten); where offsets go back, so that sequences own more tokens than there are, all may be left out; a page index outside
+ * 0 .. num_pages - 1 is left out with its tokens (FLAT_CACHE_BAD_PAGE).
  *
  * flat_attn_cache_append writes the new tokens' K, V [total, Hkv, d] bf16 (strides of token and head in elements, multiples of 8; d
  * contiguous) to their places.  The exponent of a page and head is the least e >= -117 with max |x| <= 448 * 2^e over the tokens written

@@ -11,7 +11,8 @@
 // small units an SM are better than few large ones (24 prompts of 1-4K tokens, pages of 64, d = 128: four CTAs an SM 62.9 us, eight
 // passes in two CTAs 71.6, two passes 89).  The largest magnitude is taken from the bits, two values at a time, the check for infinities
 // only where there is one (with plain comparisons twice the time).  Measured: 6 prompts, 11,700 tokens, 8 heads, d = 128 in pages of
-// 16 (72 MB) 15.5 us out of memory, 12 out of L2.
+// 16 (72 MB) 14.8 us out of memory, 11 out of L2.  A call's grid goes by its tokens, not by its longest sequence: 254 sequences with one and two with 5,596
+// new tokens 13 us in pages of 16 and 21 of 64 (a place for as many pages as the longest has, for every sequence: 367 and 392).
 // With one new token a sequence a warp takes the token's keys or values of a head: 64 sequences, 8 heads 3.1 us, which is the launch
 // and the chain.  The page that is requantised when its scale grows has eight rows in flight a lane.
 #include <cuda_bf16.h>
@@ -119,7 +120,8 @@ struct AppendArgs {
     const __nv_bfloat16* x[2];                           // K, V
     long long st[2], sh[2];
     long long total;
-    int max_new, slots;                                  // slots: pages that a sequence's new tokens may touch
+    int max_new;
+    unsigned most_pages;                                 // that the grid was made for (append_kernel)
 };
 
 // ---------------------------------------------------------------- one new token a sequence: a warp per (sequence, head, K or V)
@@ -167,18 +169,80 @@ __global__ void __launch_bounds__(256, 4)
 append_kernel(const __grid_constant__ AppendArgs p) {
     using U = Unit<D, PAGE>;
     constexpr int ROWS = U::WARPS * 32 / (D / 16);       // of a pass
-    __shared__ int tops[8];
+    __shared__ int tops[8], found[U::PER_CTA][5];        // found: sequence, its span, the page's place among those of its new tokens
+    __shared__ unsigned sums[8];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int warp = threadIdx.x >> 5, tid = threadIdx.x % (32 * U::WARPS);
-    const unsigned unit = blockIdx.x * U::PER_CTA + warp / U::WARPS, heads = p.c.Hkv, slots = p.slots;
-    const int which = unit & 1, h = (unit >> 1) % heads, slot = (unit >> 1) / heads % slots, s = (unit >> 1) / heads / slots;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x % (32 * U::WARPS);
+    const unsigned heads = p.c.Hkv;
+    // The pages that new tokens go to, sequence after sequence, are counted; unit / 2 / heads is a page's place among them.  (No more than
+    // num_seqs * max_pages: with their heads, keys and values they fit 32 bits.)
+    auto pages_of = [&](int s, Span& sp) {
+        if (!read_span(p.c, s, p.total, p.max_new, sp) || sp.n == 0) return 0u;
+        return static_cast<unsigned>((sp.len - 1) / PAGE - (sp.len - sp.n) / PAGE + 1);
+    };
+    auto before_and_this = [&](unsigned v) {             // of the lanes below and this one
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned u = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += u;
+        }
+        return v;
+    };
+    const unsigned first_unit = blockIdx.x * U::PER_CTA, unit = first_unit + warp / U::WARPS;
+    const int which = unit & 1, h = (unit >> 1) % heads;
+    int s, slot;
     Span sp{0, 0, 0};
-    bool work = s < p.c.num_seqs && read_span(p.c, s, p.total, p.max_new, sp) && sp.n > 0;
-    // (tokens before the new ones and slots for them: up to 2^30 tokens each, so that the end of the last slot passes 31 bits)
+    unsigned all_pages;
+    if (p.c.num_seqs <= 32) {                            // every warp for itself, a lane a sequence
+        const unsigned pages = lane < p.c.num_seqs ? pages_of(lane, sp) : 0, upto = before_and_this(pages), at = (unit >> 1) / heads;
+        all_pages = __shfl_sync(0xffffffffu, upto, 31);
+        s = __ffs(__ballot_sync(0xffffffffu, upto > at)) - 1;              // (-1: no such unit)
+        slot = at - __shfl_sync(0xffffffffu, upto - pages, s);
+        sp = Span{__shfl_sync(0xffffffffu, sp.q0, s), __shfl_sync(0xffffffffu, sp.n, s), __shfl_sync(0xffffffffu, sp.len, s)};
+    } else {
+        // the CTA together, a thread a few sequences (by every warp for itself: 256 sequences, two of them with 5,600 tokens, 19.6 us against 12.0;
+        // this for six sequences: 13.3 against 11.0)
+        const int per = (p.c.num_seqs + 255) / 256, s_begin = threadIdx.x * per, s_end = min(s_begin + per, p.c.num_seqs);
+        unsigned pages = 0;
+#pragma unroll 4
+        for (int i = s_begin; i < s_end; ++i) pages += pages_of(i, sp);
+        unsigned upto = before_and_this(pages);
+        if (lane == 31) sums[warp] = upto;
+        __syncthreads();
+        all_pages = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            if (w < warp) upto += sums[w];
+            all_pages += sums[w];
+        }
+        // the thread whose sequences have the page of a unit says which one it is
+#pragma unroll 1
+        for (int i = 0; i < U::PER_CTA; ++i) {
+            const unsigned at = ((first_unit + i) >> 1) / heads;
+            unsigned before = upto - pages;
+            if (at < before || at >= upto) continue;
+            int whose = s_begin;
+            if (per > 1)                                 // (one sequence a thread: it has been read)
+                for (unsigned n = pages_of(whose, sp); at >= before + n; n = pages_of(++whose, sp)) before += n;
+            found[i][0] = whose; found[i][1] = sp.q0; found[i][2] = sp.n; found[i][3] = sp.len; found[i][4] = at - before;
+        }
+        __syncthreads();
+        const int mine = warp / U::WARPS;
+        s = found[mine][0];
+        slot = found[mine][4];
+        sp = Span{found[mine][1], found[mine][2], found[mine][3]};
+    }
+    const unsigned units = 2 * heads * all_pages;
+    if (first_unit >= units) return;                     // (the whole CTA)
+    if (all_pages > p.most_pages) {                      // (offsets that go back and forth: more tokens than there are)
+        if (p.c.status && threadIdx.x == 0) atomicExch(p.c.status, FLAT_CACHE_BAD_LENGTH);
+        return;
+    }
+    bool work = unit < units;
     const int start = sp.len - sp.n, first_page = start / PAGE, index = first_page + slot;
     int page_id = 0;
-    work = work && static_cast<unsigned>(index) * PAGE < static_cast<unsigned>(sp.len) && read_page(p.c, s, index, page_id);
+    work = work && read_page(p.c, s, index, page_id);
     const int r0 = slot == 0 ? start - first_page * PAGE : 0;
     const int r1 = !work ? 0 : sp.len - index * PAGE < PAGE ? sp.len - index * PAGE : PAGE;
     const int row = tid / (D / 16), col = tid % (D / 16) * 16;
@@ -203,7 +267,7 @@ append_kernel(const __grid_constant__ AppendArgs p) {
     for (int i = 0; i < U::PASSES; ++i) largest16(a[i], b[i], top, all);
     int most = warp_largest(top, all);
     if (U::WARPS > 1) {
-        if ((threadIdx.x & 31) == 0) tops[warp] = most;
+        if (lane == 0) tops[warp] = most;
         __syncthreads();                                 // (and every thread has read the exponent)
 #pragma unroll
         for (int w = 0; w < U::WARPS; ++w) {
@@ -226,7 +290,8 @@ append_kernel(const __grid_constant__ AppendArgs p) {
 }
 
 template <int D>
-int launch_d(const AppendArgs& p, cudaStream_t st) {
+int launch_d(const AppendArgs& args, cudaStream_t st) {
+    AppendArgs p = args;
     cudaLaunchConfig_t cfg = {};
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -241,12 +306,15 @@ int launch_d(const AppendArgs& p, cudaStream_t st) {
         cfg.blockDim = dim3(128);
     } else {
         const int per_cta = p.c.page == 16 ? Unit<D, 16>::PER_CTA : p.c.page == 32 ? Unit<D, 32>::PER_CTA : p.c.page == 64 ? Unit<D, 64>::PER_CTA : Unit<D, 128>::PER_CTA;
-        blocks = (static_cast<int64_t>(p.c.num_seqs) * p.c.Hkv * p.slots * 2 + per_cta - 1) / per_cta;
+        // Pages that new tokens may go to: those of the longest for every sequence, or as many as all tokens fill and two more a sequence
+        const int64_t longest = (p.max_new + static_cast<int64_t>(p.c.page) - 2) / p.c.page + 1;
+        const int64_t most = p.total / p.c.page + 2 * static_cast<int64_t>(p.c.num_seqs), pages = longest < most / p.c.num_seqs ? longest * p.c.num_seqs : most;
+        p.most_pages = static_cast<unsigned>(pages < 0xffffffffll ? pages : 0xffffffffll);
+        blocks = (pages * p.c.Hkv * 2 + per_cta - 1) / per_cta;
         cfg.blockDim = dim3(256);
         kern = p.c.page == 16 ? append_kernel<D, 16> : p.c.page == 32 ? append_kernel<D, 32> : p.c.page == 64 ? append_kernel<D, 64> : append_kernel<D, 128>;
     }
-    if (blocks > 0x0fffffff) return FLAT_ERR_SHAPE;      // (units, up to eight to a CTA, are counted in 31 bits)
-    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));  // (2^34 tokens and heads of a cache are at most 2^30 CTAs)
     return cudaLaunchKernelEx(&cfg, kern, p) == cudaSuccess ? FLAT_OK : FLAT_ERR_CUDA;
 }
 
@@ -255,7 +323,7 @@ int launch_d(const AppendArgs& p, cudaStream_t st) {
 int launch_cache_append(const flat_attn_cache_t& c, const void* K, const void* V, int64_t total, long long k_st, long long k_sh,
                         long long v_st, long long v_sh, int max_new, cudaStream_t st) {
     AppendArgs p{cache_view(c), {static_cast<const __nv_bfloat16*>(K), static_cast<const __nv_bfloat16*>(V)}, {k_st, v_st}, {k_sh, v_sh},
-                 total, max_new, static_cast<int>((max_new + static_cast<int64_t>(c.page) - 2) / c.page + 1)};
+                 total, max_new, 0};
     return c.d == 64 ? launch_d<64>(p, st) : launch_d<128>(p, st);
 }
 

@@ -153,3 +153,65 @@ def test_least_scale_over_many_keys(api, new, longest):
     err, up = (O.double() - R).abs(), 2.0 ** 117
     assert (err * up <= (2.0 ** -8 * R.abs() + (2.0 ** -10 + 2 * logits[..., None] + more) * A) * up).all(), float((err / A).max())
     assert ((lse.double() - (L + math.log(longest // page))).abs() <= logits + 2.0 ** -18 * (1 + 20) + more).all()
+
+
+# ---------------------------------------------------------------- appending
+
+def check_append(api, gen, cu, lens, good, most, Hkv, page, d, T, code=0):
+    """Appending with offsets `cu` of which only the sequences `good` are right, against the plain form, bit by bit."""
+    k, v, ke, ve, table = ref.make_cache(gen, lens, Hkv, page, d, "cuda")
+    K, V = (torch.randn(T, Hkv, d, generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+    want = [t.clone() for t in (k, v, ke, ve)]
+    for s in good:
+        for x, c, e in ((K, want[0], want[2]), (V, want[1], want[3])):
+            ref.append(x[cu[s]:cu[s + 1]].double(), c, e, table[s:s + 1].tolist(), [0, cu[s + 1] - cu[s]], [lens[s]])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.flat_attn_cache_append(K, V, k, v, ke, ve, table, ints(cu), ints(lens), most, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == code
+    for got, w in zip((k, v, ke, ve), want):
+        assert torch.equal(got.view(torch.uint8), w.view(torch.uint8))
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (128, 128), (64, 32)])
+def test_append_prompts_among_single_tokens(api, d, page):
+    gen, S = torch.Generator().manual_seed(25), 140
+    new = [1] * S
+    new[17], new[90], new[139], new[5], new[60] = 1000, 333, 48, 0, 0
+    lens = [n + int(x) for n, x in zip(new, torch.randint(0, 200, (S,), generator=gen))]
+    check_append(api, gen, [c + 3 for c in ref.offsets(new)], lens, range(S), 1000, 2, page, d, sum(new) + 8)
+
+
+def test_append_beside_sequences_that_do_not_fit(api):
+    """Offsets that go back, more new tokens than announced or than the sequence is long: those sequences are left out, the others are not."""
+    gen = torch.Generator().manual_seed(26)
+    cu, lens = [0, 20, 19, 60, 90, 95, 300, 310, 330, 320], [40, 30, 50, 25, 20, 400, 15, 64, 9]
+    #   new:       20, -1, 41, 30 > length, 5, 205 > most, 10, 20, -10
+    check_append(api, gen, cu, lens, [0, 2, 4, 6, 7], 50, 2, 16, 64, 330, api.FLAT_CACHE_BAD_LENGTH)
+
+
+def test_append_of_tokens_owned_twice(api):
+    """Offsets that go back so far that the sequences own more tokens than there are: said, and nothing is written."""
+    gen = torch.Generator().manual_seed(29)
+    cu, lens = [0, 500] * 20, [500] * 39
+    check_append(api, gen, cu, lens, [], 500, 1, 16, 64, 500, api.FLAT_CACHE_BAD_LENGTH)
+
+
+def test_append_with_room_for_many_pages_of_many_heads(api):
+    """As many pages and heads as a cache may have, few of them with new tokens: no number of possible places is refused."""
+    gen = torch.Generator().manual_seed(27)
+    Hkv, d, page, n, longest = 512, 64, 16, 21, 1 << 25
+    k, v, ke, ve, _ = ref.make_cache(gen, [48], Hkv, page, d, "cuda", spare=0)
+    table = torch.full((1, longest // page), 2, dtype=torch.int32, device="cuda")
+    table[0, -2:] = ints([0, 1])
+    x = torch.randn(1, Hkv, d, generator=gen).to(torch.bfloat16).cuda()
+    want = [t.clone() for t in (k, v, ke, ve)]
+    for i in range(2):                                   # (the last 21 of the 32 tokens of a sequence of two pages)
+        ref.append(x.double().expand(n, Hkv, d), want[i], want[2 + i], [[0, 1]], [0, n], [32])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    many = x.expand(longest, Hkv, d)
+    api.flat_attn_cache_append(many, many, k, v, ke, ve, table, ints([0, n]), ints([longest]), longest, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    for got, w in zip((k, v, ke, ve), want):
+        assert torch.equal(got.view(torch.uint8), w.view(torch.uint8))

@@ -155,6 +155,32 @@ def test_least_scale_over_many_keys(api, new, longest):
     assert ((lse.double() - (L + math.log(longest // page))).abs() <= logits + 2.0 ** -18 * (1 + 20) + more).all()
 
 
+# ---------------------------------------------------------------- forms that only large batches take
+
+@pytest.mark.parametrize("d,page,G,n", [(128, 64, 1, 1), (128, 16, 4, 1), (128, 16, 5, 3), (128, 128, 8, 4), (64, 64, 2, 1), (64, 128, 1, 2), (64, 32, 7, 4),
+                                        (64, 128, 5, 2)])
+def test_items_dealt_to_single_warps(api, sms, d, page, G, n):
+    """At least twelve items an SM: shares that begin and end inside items, some of them longer than a share."""
+    gen, Hkv = torch.Generator().manual_seed(24), 8
+    seqs = -(-12 * sms // (Hkv * -(-n * G // 16))) + 3
+    lens = [n + int(x) for x in torch.randint(0, 400, (seqs,), generator=gen)]
+    lens[seqs // 2], lens[-1] = 5000, n
+    check_call(api, gen, workspace(api, G * Hkv, Hkv, d), [n] * seqs, lens, G, Hkv, page, d, times=2)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("seqs,most", [(40, 300), (100, 90)])
+def test_prompts_of_many_sequences(api, d, seqs, most):
+    """More sequences than a warp has lanes, prompts, single tokens and sequences without new tokens among them."""
+    gen = torch.Generator().manual_seed(seqs)
+    new = [int(x) for x in torch.randint(0, most, (seqs,), generator=gen)]
+    new[3::7] = [1] * len(new[3::7])
+    new[5::11] = [0] * len(new[5::11])
+    lens = [n + int(x) for n, x in zip(new, torch.randint(0, 700, (seqs,), generator=gen))]
+    lens[seqs // 2] += 6000
+    check_call(api, gen, workspace(api, 6, 2, d), new, lens, 3, 2, 32, d, times=2)
+
+
 # ---------------------------------------------------------------- appending
 
 def check_append(api, gen, cu, lens, good, most, Hkv, page, d, T, code=0):

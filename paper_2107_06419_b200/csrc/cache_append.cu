@@ -12,7 +12,7 @@
 // passes in two CTAs 71.6, two passes 89).  The largest magnitude is taken from the bits, two values at a time, the check for infinities
 // only where there is one (with plain comparisons twice the time).  Measured: 6 prompts, 11,700 tokens, 8 heads, d = 128 in pages of
 // 16 (72 MB) 14.8 us out of memory, 11 out of L2.  A call's grid goes by its tokens, not by its longest sequence: 254 sequences with one and two with 5,596
-// new tokens 13 us in pages of 16 and 21 of 64 (a place for as many pages as the longest has, for every sequence: 367 and 392).
+// new tokens together 13 us in pages of 16 and 21 of 64 (a place for as many pages as the longest has, for every sequence: 367 and 392).
 // With one new token a sequence a warp takes the token's keys or values of a head: 64 sequences, 8 heads 3.1 us, which is the launch
 // and the chain.  The page that is requantised when its scale grows has eight rows in flight a lane.
 #include <cuda_bf16.h>

@@ -14,8 +14,8 @@
 // rows) 176, with conversions through the header's structures (two more instructions for two values) 215.  What is left where an
 // item is short is the chain of a part -- table entry, tokens, products, join, about 3 us -- and 2 us of deal: one sequence of 2,000 tokens
 // 8.8 us, 16 sequences of 2-8K with 16 heads of 64 in pages of sixteen 31.8 (4.0 TB/s).  With two row groups twelve warps an SM do not cover
-// the chain of a chunk (750 instructions): 12 sequences of 4-32K, 4 key heads, 28 rows in two tiles 91 us (2.5 TB/s of the cache read
-// once).
+// the chain of a chunk (750 instructions): 12 sequences of 4-32K, 4 key heads, 28 rows in two tiles 92 us (2.5 TB/s of the cache read
+// once); those forms spill 24 to 88 bytes.
 //
 // Work is dealt by chunks of 8 KB (keys and values of 32 tokens, d = 128): all chunks of all (sequence, key head, row tile) in one
 // row, an equal share of neighbouring chunks to each team, or, where there are few items, a part of one item each.  A team is a

@@ -19,7 +19,8 @@
 // for the tensor pipe (A of the logits alone 512) and 512 of conversions; its exponentials take 1,010 cycles of the exponent unit;
 // measured 1,750 cycles (of 1,920 in an earlier form the softmax took 1,270 to work and 330 to wait for logits).  4,096 queries behind
 // 28,672 tokens, 32 heads on 8: 1,580 us in the first 20 ms of launches (1,305 TFLOP/s), 1,830 at the power cap (1,120; a cuBLAS GEMM
-// 1,639 and 1,396).  d = 64: the exponentials, 580 TFLOP/s.  How long a step takes also depends on the code around it: with masked steps in a
+// 1,639 and 1,396).  d = 64: 580 TFLOP/s, by the softmax warps, a thread a row, two warps a scheduler, which load, compute, store and wait in turn: 1,250 of
+// 1,700 cycles a step at work (the exponent unit 900).  How long a step takes also depends on the code around it: with masked steps in a
 // loop instead of unrolled 128 items of d = 128 take 480 us against 488.  Tried, on 128 items: the converters' own cp.async (their addresses
 // were half of a step: 587 us against 522), logits of two steps in one product (N = 128, one buffer a tile: 567 against 522; d = 64 494
 // against 466), no polynomial 524 and one in sixteen 524 against 512, one in four 513 (d = 64 456 against 459).

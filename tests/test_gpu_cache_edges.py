@@ -111,6 +111,32 @@ def test_nan_where_items_are_dealt_to_single_warps(api, sms, d, page, G, n):
     attend_with_nan(api, torch.Generator().manual_seed(22), [n] * seqs, lens, G, page, d, True)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,new,lens", [(4, [1, 1], [300, 40]), (2, [4, 1], [500, 77]), (2, [150, 90], [1500, 90])])
+def test_queries_that_are_not_finite(api, d, G, new, lens):
+    """Rows with NaN or infinite features are NaN, but for those whose logits are all -inf: like rows that see nothing, they are 0 and lse
+    -inf, as everywhere in the library.  The other rows are as without them."""
+    gen, Hkv, page, cu = torch.Generator().manual_seed(30), 2, 32, ref.offsets(new)
+    k, v, ke, ve, table = ref.make_cache(gen, lens, Hkv, page, d, "cuda")
+    Q = torch.randn(cu[-1], G * Hkv, d, generator=gen).to(torch.bfloat16).cuda()
+    R, L, A, B = ref.attention(Q, k, v, ke, ve, table, cu, lens, 0.1, True)
+    nan, none = (torch.zeros(Q.shape[:2], dtype=torch.bool, device="cuda") for _ in range(2))
+    for i, (row, head, value) in enumerate([(0, 1, math.nan), (cu[1], 0, math.inf), (cu[-1] - 1, G * Hkv - 1, -math.inf), (cu[1] // 2, G, math.nan)]):
+        Q[row, head, 7 * i + 3] = value
+        s = 0 if row < cu[1] else 1
+        ids = [int(p) for p in table[s][:-(-lens[s] // page)]]
+        keys = ref.values(k, ke, ids, lens[s], head // G)[:row - cu[s] + lens[s] - new[s] + 1]
+        x = (Q[row, head].double() * keys).sum(1)
+        (none if (x == -math.inf).all() else nan)[row, head] = True
+    O, lse = torch.full_like(Q, 7.0), torch.full(Q.shape[:2], 7.0, device="cuda")
+    api.flat_attn_cache_fwd(Q, O, k, v, ke, ve, table, ints(cu), ints(lens), max(new), 0.1, workspace(api, G * Hkv, Hkv, d), causal=True, lse=lse)
+    torch.cuda.synchronize()
+    assert torch.isnan(O[nan]).all() and torch.isnan(lse[nan]).all()
+    assert (O[none] == 0).all() and (lse[none] == -math.inf).all()
+    bad = nan | none
+    ref.check_attention(torch.where(bad[..., None], R, O.double()), torch.where(bad, L, lse.double()), (R, L, A, B), d)
+
+
 # ---------------------------------------------------------------- scales at the ends of the range
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -241,3 +267,48 @@ def test_append_with_room_for_many_pages_of_many_heads(api):
     assert int(status) == 0
     for got, w in zip((k, v, ke, ve), want):
         assert torch.equal(got.view(torch.uint8), w.view(torch.uint8))
+
+
+# ---------------------------------------------------------------- one call after another
+
+@pytest.mark.parametrize("d,page,Hkv,new,lens", [(128, 64, 4, [70, 1, 1, 30, 1] + [1] * 40, [2000, 9000, 40, 333, 5000] + [400 + 30 * i for i in range(40)]),
+                                                 (64, 16, 2, [30, 1, 1, 1], [60, 90, 40, 300])])
+def test_inputs_that_change_from_call_to_call(api, d, page, Hkv, new, lens):
+    """Rotation, append and a mixed batch's attention again and again on the same buffers, other tokens and lengths each time: without a wait in
+    between, and in a graph, the bits are those of calls that are waited for."""
+    gen, G, N = torch.Generator().manual_seed(31), 4, 6
+    cu, T = ref.offsets(new), sum(new)
+    cache = ref.make_cache(gen, lens, Hkv, page, d, "cuda")
+    saved = [t.clone() for t in cache[:4]]
+    tokens = [[(torch.randn(T, h, d, generator=gen) * 2.0 ** (i % s)).to(torch.bfloat16).cuda() for h, s in ((G * Hkv, 1), (Hkv, N), (Hkv, 3))] for i in range(N)]
+    lengths = [ints(lens), ints([m - (m > n + 5) for n, m in zip(new, lens)])]
+    rope, _ = api.flat_attn_rope_table(d)
+    at, dcu, dlens, work = ints([m - n + i for n, m in zip(new, lens) for i in range(n)]), ints(cu), ints(lens), workspace(api, G * Hkv, Hkv, d)
+    Q, K, outs = torch.empty_like(tokens[0][0]), torch.empty_like(tokens[0][1]), [torch.empty_like(tokens[0][0]) for _ in range(N)]
+
+    def steps(wait):
+        for i, (q, k, v) in enumerate(tokens):
+            dlens.copy_(lengths[i % 2])
+            api.flat_attn_rope_fwd(q, k, rope, Q, K, positions=at)
+            wait()
+            api.flat_attn_cache_append(K, v, *cache, dcu, dlens, max(new))
+            wait()
+            api.flat_attn_cache_fwd(Q, outs[i], *cache, dcu, dlens, max(new), 0.1, work, causal=True)
+            wait()
+
+    def again():
+        for a, b in zip(cache, saved):
+            a.view(torch.uint8).copy_(b.view(torch.uint8))
+        for o in outs:
+            o.zero_()
+    steps(torch.cuda.synchronize)
+    want = [o.clone() for o in outs]
+    again()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        steps(lambda: None)
+    for run in [lambda: steps(lambda: None), graph.replay] * 20:
+        again()
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
